@@ -261,6 +261,111 @@ spd_status spd_semiring_pairwise(spd_handle *handle, const spd_csr *A, const spd
 spd_status spd_semiring_knn(spd_handle *handle, const spd_csr *Q, const spd_csr *Index,
                             const spd_semiring *semiring, int k, int64_t *out_idx, float *out_dist);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Attention over a paged cache: what a program that answers from the passages spd_knn found does next.
+ * Keys and values lie in pages of `page_size` tokens; a request's tokens are the pages its row of the block table names, in
+ * order.  Per step: spd_paged_plan (tables, slots and positions of the new tokens, from the lengths), spd_paged_append (their keys
+ * and values into the cache), and spd_paged_attention or spd_paged_sparse_attention (the new tokens' queries over their pages).
+ *
+ * Conventions, beside those above
+ *  - Every array is on the DEVICE.  No call reads anything back or waits: lengths and tables are looked at by the kernels, so
+ *    the calls can be captured into a graph once the scratch is there (a first call, or spd_set_workspace with
+ *    spd_paged_workspace_bytes).  The sizes in the structs are the arrays' and bound every access: lengths and tables that
+ *    contradict them give fewer tokens or masked ones, and never an access outside.
+ *  - A page number outside [0, n_pages) in a block table is a page that is not there: its tokens are masked, and
+ *    a new token of it is dropped.  What lies past a request's length, or in pages that no table names, may hold anything, NaN too.
+ *    Queries, and keys and values of a request's tokens, must be finite.
+ *  - Products of 16-bit values are summed in fp32, and so are the softmax's sums; weights exp(logit - running maximum) are rounded to the
+ *    cache's type for their product with the values, and `out` is rounded once.  Equal calls give equal bits. */
+typedef enum { SPD_BF16 = 0, SPD_F16, SPD_DTYPE_COUNT } spd_dtype;
+
+/* page, token in it, key head and place of an element of k: k[page * page_stride + token * token_stride + head * head_stride + place],
+ * and of v alike.  Strides are in elements, multiples of 8 (heads may lie before tokens), arrays 16-byte aligned. */
+typedef struct {
+    spd_dtype dtype;
+    int32_t page_size;      /* tokens to a page: a power of two from 16 to 1024 */
+    int32_t n_kv_heads;
+    int32_t head_dim;       /* 64 or 128 */
+    int64_t n_pages;
+    void *k, *v;
+    int64_t page_stride, token_stride, head_stride;
+    /* What spd_paged_sparse_attention scores pages by, contiguous; NULL (all three) in a cache that does without.  In each place the least
+     * [0] and the greatest [1] value of the page's keys, and the same as 8-bit codes of one scale to a page and head:
+     * scale = greatest magnitude * (1/127 in fp32), code = bounds / scale rounded to the nearest whole number (ties to even). */
+    void *bounds;           /* [n_pages][n_kv_heads][2][head_dim], dtype */
+    int8_t *codes;          /* [n_pages][n_kv_heads][2][head_dim]        */
+    float *code_scale;      /* [n_pages][n_kv_heads]                     */
+} spd_paged_cache;
+
+/* A step's requests.  Request r's new tokens are rows query_start[r] .. query_start[r+1]-1 of the queries; with
+ * them it has kv_lens[r] tokens in the cache, and new token i of n stands at position kv_lens[r] - n + i.  Rows of the queries outside
+ * every request are not written. */
+typedef struct {
+    int64_t n_requests, n_tokens;   /* rows of the queries */
+    int64_t max_pages;              /* columns of the block table */
+    const int32_t *query_start;     /* n_requests + 1, non-decreasing, within [0, n_tokens] */
+    const int32_t *kv_lens;         /* n_requests */
+    const int32_t *block_table;     /* n_requests rows, table_stride apart */
+    int64_t table_stride;
+} spd_paged_batch;
+
+/* Rows of heads: element d of a token's head at ptr[token * token_stride + head * head_stride + d], the cache's type; strides are
+ * multiples of 8, the pointer 16-byte aligned (a slice of one projection's output serves). */
+typedef struct { const void *ptr; int64_t token_stride, head_stride; } spd_rows;
+
+/* Request r has past_lens[r] cached tokens and gets new_lens[r] more (negative lengths count as 0).  Writes
+ *   block_table   (in place) entries from ceil(past/page_size) up to ceil((past+new)/page_size): the next page numbers of `free_pages`,
+ *                 the requests in order; -1 where these have run out; columns past max_pages are not taken for
+ *   query_start, kv_lens   as spd_paged_batch has them
+ *   slots         n_tokens of them: page number * page_size + place in the page of every new token; -1 where there is no page, and
+ *                 past the last new token (n_tokens may be more than there are, as in a captured graph; tokens past it are dropped)
+ *   positions     n_tokens: each new token's position in its request; -1 past the last one
+ *   counts        3: new tokens, pages taken, pages that were wanting
+ * The sum of new_lens, and each past + new, must be below 2^31. */
+typedef struct {
+    int64_t n_requests, n_tokens, max_pages, n_free;
+    int32_t page_size;
+    const int32_t *past_lens, *new_lens;   /* n_requests */
+    const int32_t *free_pages;             /* n_free     */
+    int32_t *block_table;
+    int64_t table_stride;
+    int32_t *query_start, *kv_lens;
+    int64_t *slots;
+    int32_t *positions, *counts;
+} spd_paged_step;
+#define SPD_PAGED_MAX_REQUESTS 16384
+spd_status spd_paged_plan(spd_handle *handle, const spd_paged_step *step);
+
+/* Row t of `k_new` and `v_new` (n_tokens x n_kv_heads x head_dim) goes to slots[t]; a slot outside the cache drops the row.  Where the cache has
+ * bounds, those of every page that gets a key are brought up to date: a run of rows t, t+1, ... with slots one after the other in one page merges into the
+ * page's bounds, and begins them anew where it begins at the page's first slot.  So a page's keys are to come in order, and
+ * the rows of one page next to each other, as spd_paged_plan numbers them; two rows with one slot, or two runs in one page, leave either's values. */
+spd_status spd_paged_append(spd_handle *handle, const spd_paged_cache *cache, int64_t n_tokens, const spd_rows *k_new,
+                            const spd_rows *v_new, const int64_t *slots);
+
+/* Device scratch that one call of spd_paged_attention (`n_select` = 0) or spd_paged_sparse_attention with these sizes needs at most. */
+spd_status spd_paged_workspace_bytes(const spd_handle *handle, const spd_paged_cache *cache, const spd_paged_batch *batch,
+                                     int n_heads, int n_select, size_t *bytes);
+
+/* out[t][h] = sum over j of softmax(scale * q[t][h] . k_j) v_j, j over the positions up to t's own of its request, in key head
+ * h / (n_heads / n_kv_heads); contiguous, n_tokens x n_heads x head_dim, the cache's type.  lse[t][h] (fp32, NULL if it is not wanted) = the
+ * natural logarithm of the sum of exp(scale * q . k_j).  A token without any such position gets 0 and -infinity.
+ * `n_heads` is a multiple of n_kv_heads, `scale` finite and positive. */
+spd_status spd_paged_attention(spd_handle *handle, const spd_paged_cache *cache, const spd_paged_batch *batch, const spd_rows *q,
+                               int n_heads, float scale, void *out, float *lse);
+
+/* Attention over `n_select` pages of each token and key head.  A page's score bounds the logits of its keys: with lo <= k <= hi in every place,
+ * q . k is at most sum max(q,0) hi - max(-q,0) lo.  The queries of a key head, whose heads share the selection, are rounded to 8-bit codes of one scale (their
+ * greatest magnitude * (1/127)), u = the sum over the heads of max(code, 0) and w of max(-code, 0), each times 1/(number of heads) and rounded to a
+ * whole number, all in fp32, and score = (sum u hi - w lo over the page's codes) * code_scale: whole numbers with one rounding, the same however they are summed.
+ * Selected are the request's first page, the token's own, and the others before it by the greatest score, equal ones by the
+ * lower place in the request.  selected[t][j] ([n_tokens][n_kv_heads][n_select]) holds their places in the request (columns of the block table),
+ * ascending, then -1.  `n_select` from 2 to SPD_PAGED_MAX_SELECT.  out and lse as above, over the selected pages. */
+#define SPD_PAGED_MAX_SELECT 64
+spd_status spd_paged_sparse_attention(spd_handle *handle, const spd_paged_cache *cache, const spd_paged_batch *batch,
+                                      const spd_rows *q, int n_heads, float scale, int n_select, int32_t *selected, void *out,
+                                      float *lse);
+
 /* Device pass over a matrix that checks what the other calls assume: row pointers start
  * at 0, never decrease and end at nnz; columns ascend strictly inside a row and lie in
  * [0, n_cols); values are finite (and, if `require_nonnegative`, not negative).

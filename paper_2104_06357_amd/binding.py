@@ -46,6 +46,31 @@ class SemiringStruct(ctypes.Structure):
                 ("transform", ctypes.c_int), ("epilogue", ctypes.c_int)]
 
 
+class PagedCacheStruct(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("n_pages", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("bounds", ctypes.c_void_p),
+                ("codes", ctypes.c_void_p), ("code_scale", ctypes.c_void_p)]
+
+
+class PagedBatchStruct(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                ("query_start", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64)]
+
+
+class RowsStruct(ctypes.Structure):
+    _fields_ = [("ptr", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class PagedStepStruct(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int64), ("n_tokens", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("n_free", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("past_lens", ctypes.c_void_p), ("new_lens", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("query_start", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("counts", ctypes.c_void_p)]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 24), ("rows_per_group", ctypes.c_int32), ("staging_kind", ctypes.c_int32),
                 ("block", ctypes.c_int32), ("lds_bytes", ctypes.c_int32), ("a_rows", ctypes.c_int64),
@@ -78,6 +103,12 @@ def lib():
         L.spd_index_destroy.argtypes = [vp, vp]
         L.spd_index_pairwise.argtypes = [vp, csr_p, vp, vp]
         L.spd_index_knn.argtypes = [vp, csr_p, vp, i32, vp, vp]
+        rows_p, cache_p, batch_p = (ctypes.POINTER(t) for t in (RowsStruct, PagedCacheStruct, PagedBatchStruct))
+        L.spd_paged_plan.argtypes = [vp, ctypes.POINTER(PagedStepStruct)]
+        L.spd_paged_append.argtypes = [vp, cache_p, i64, rows_p, rows_p, vp]
+        L.spd_paged_workspace_bytes.argtypes = [vp, cache_p, batch_p, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        L.spd_paged_attention.argtypes = [vp, cache_p, batch_p, rows_p, i32, f32, vp, vp]
+        L.spd_paged_sparse_attention.argtypes = [vp, cache_p, batch_p, rows_p, i32, f32, i32, vp, vp, vp]
         L.spd_csr_validate.argtypes = [vp, csr_p, i32]
         L.spd_set_option.argtypes = [vp, ctypes.c_char_p, i64]
         L.spd_last_error.argtypes = [vp]
@@ -93,7 +124,8 @@ def lib():
         for fn in ("spd_create", "spd_destroy", "spd_workspace_bytes", "spd_set_workspace", "spd_pairwise",
                    "spd_pairwise_static",
                    "spd_knn", "spd_semiring_pairwise", "spd_semiring_knn", "spd_index_create", "spd_index_destroy",
-                   "spd_index_pairwise", "spd_index_knn", "spd_csr_validate", "spd_set_option", "spd_host_pair_value",
+                   "spd_index_pairwise", "spd_index_knn", "spd_paged_plan", "spd_paged_append", "spd_paged_workspace_bytes",
+                   "spd_paged_attention", "spd_paged_sparse_attention", "spd_csr_validate", "spd_set_option", "spd_host_pair_value",
                    "spd_host_plan_summary", "spd_host_list_plan"):
             getattr(L, fn).restype = ctypes.c_int
         _lib = L
@@ -140,6 +172,83 @@ class DeviceCsr:
                          self.indices.data_ptr() if self.nnz else None,
                          self.values.data_ptr() if self.nnz else None,
                          self.host_indptr.ctypes.data if self.host_indptr is not None else None)
+
+
+def _rows(x, heads, cache, name):
+    """A (tokens, heads, head_dim) tensor of the cache's type as spd_rows: any strides of tokens and heads."""
+    if x.dtype != cache.k.dtype or x.device != cache.k.device:
+        raise ValueError("%s must have the cache's type and device" % name)
+    if x.dim() != 3 or x.shape[2] != cache.k.shape[3] or (heads and x.shape[1] != heads):
+        raise ValueError("%s must be (tokens, %s, %d)" % (name, heads or "heads", cache.k.shape[3]))
+    stride = x.stride()
+    if stride[2] != 1 and x.numel():
+        raise ValueError("the places of a head must lie next to each other in %s" % name)
+    return RowsStruct(x.data_ptr(), stride[0], stride[1])
+
+
+def _out(x, shape, dtype, device, name):
+    import torch
+    if x is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if x.dtype != dtype or x.device != device or tuple(x.shape) != shape or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %s on %s" % (name, dtype, shape, device))
+    return x
+
+
+def _int32(x, dims, device, name):
+    import torch
+    if x.dtype != torch.int32 or x.dim() != dims or x.device != device or (x.numel() and x.stride(-1) != 1):
+        raise ValueError("%s must be a %d-dimensional int32 tensor on %s, its last dimension without gaps" % (name, dims, device))
+    return x
+
+
+class PagedCache:
+    """Keys and values in pages: `k` and `v` are (pages, page_size, heads, head_dim) tensors of one type (bfloat16 or float16), of
+    any strides, the same of both, whose last is 1 (heads may lie before tokens: pass a transposed view).  `bounds`
+    (pages, heads, 2, head_dim), `codes` (the same, int8) and `code_scale` (pages, heads, float32) are what
+    paged_sparse_attention selects pages by; bounds=True makes them, for a cache that is empty."""
+
+    def __init__(self, k, v, bounds=None, codes=None, code_scale=None):
+        import torch
+        dtypes = {torch.bfloat16: 0, torch.float16: 1}                       # spd_dtype
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in dtypes or k.device != v.device or not k.is_cuda:
+            raise ValueError("k and v must be (pages, page_size, heads, head_dim) tensors of one 16-bit type on the GPU")
+        if k.stride() != v.stride() or (k.stride(3) != 1 and k.numel()):
+            raise ValueError("k and v must have the same strides, the last of them 1")
+        pages, page, heads, dim = k.shape
+        if bounds is True:
+            bounds, codes = (torch.zeros((pages, heads, 2, dim), dtype=t, device=k.device) for t in (k.dtype, torch.int8))
+            code_scale = torch.zeros((pages, heads), dtype=torch.float32, device=k.device)
+        kept = (bounds, codes, code_scale)
+        if any(x is not None for x in kept):
+            if any(x is None for x in kept):
+                raise ValueError("bounds, codes and code_scale go together")
+            for x, shape, dtype in zip(kept, ((pages, heads, 2, dim), (pages, heads, 2, dim), (pages, heads)),
+                                       (k.dtype, torch.int8, torch.float32)):
+                _out(x, shape, dtype, k.device, "bounds, codes or code_scale")
+        self.k, self.v, self.bounds, self.codes, self.code_scale = k, v, bounds, codes, code_scale
+        at = [x.data_ptr() if x is not None else None for x in kept]
+        self._struct = PagedCacheStruct(dtypes[k.dtype], page, heads, dim, pages, k.data_ptr(), v.data_ptr(), k.stride(0),
+                                        k.stride(1), k.stride(2), *at)
+        self._ref = ctypes.byref(self._struct)
+
+
+class PagedBatch:
+    """A step's requests: `query_start` (n + 1), `kv_lens` (n) and `block_table` (n, columns), int32 on the GPU.  From
+    Handle.paged_plan also `slots` (int64), `positions` and `counts` of the new tokens."""
+
+    def __init__(self, query_start, kv_lens, block_table):
+        _int32(query_start, 1, block_table.device, "query_start")
+        _int32(kv_lens, 1, block_table.device, "kv_lens")
+        _int32(block_table, 2, block_table.device, "block_table")
+        n = kv_lens.shape[0]
+        if not block_table.is_cuda or query_start.shape[0] != n + 1 or block_table.shape[0] != n:
+            raise ValueError("query_start, kv_lens and block_table must be of n + 1, n and n requests, on the GPU")
+        self.query_start, self.kv_lens, self.block_table = query_start, kv_lens, block_table
+        self.slots = self.positions = self.counts = None
+        self._struct = PagedBatchStruct(n, 0, block_table.shape[1], query_start.data_ptr(), kv_lens.data_ptr(),
+                                        block_table.data_ptr(), block_table.stride(0))
+        self._ref = ctypes.byref(self._struct)
 
 
 class Handle:
@@ -277,6 +386,78 @@ class Handle:
                                                out_idx.data_ptr() if out_idx.numel() else None,
                                                out_dist.data_ptr() if out_dist.numel() else None))
         return out_idx, out_dist
+
+    def paged_plan(self, past_lens, new_lens, free_pages, block_table, page_size: int, n_tokens: int, out=None) -> PagedBatch:
+        """Block table (in place), slots and positions of a step's new tokens, from the requests' lengths, on the GPU
+        (spd_paged_plan).  `n_tokens`: how many new tokens there are, or more; `out`: a PagedBatch of an earlier step with the same
+        sizes, whose tensors are written again."""
+        import torch
+        device, n = block_table.device, past_lens.shape[0]
+        for x, dims, name in ((past_lens, 1, "past_lens"), (new_lens, 1, "new_lens"), (free_pages, 1, "free_pages"),
+                              (block_table, 2, "block_table")):
+            _int32(x, dims, device, name)
+        if not block_table.is_cuda or new_lens.shape[0] != n or block_table.shape[0] != n:
+            raise ValueError("past_lens, new_lens and block_table must be of the same requests, on the GPU")
+        if out is None:
+            i32 = {"dtype": torch.int32, "device": device}
+            out = PagedBatch(torch.empty(n + 1, **i32), torch.empty(n, **i32), block_table)
+            out.slots = torch.empty(n_tokens, dtype=torch.int64, device=device)
+            out.positions, out.counts = torch.empty(n_tokens, **i32), torch.empty(3, **i32)
+        elif out.slots is None or out.slots.shape[0] != n_tokens or out.kv_lens.shape[0] != n or out.block_table is not block_table:
+            raise ValueError("out must be a PagedBatch that paged_plan made for this block table and these sizes")
+        step = PagedStepStruct(n, n_tokens, block_table.shape[1], free_pages.shape[0], int(page_size), past_lens.data_ptr(),
+                               new_lens.data_ptr(), free_pages.data_ptr(), block_table.data_ptr(), block_table.stride(0),
+                               out.query_start.data_ptr(), out.kv_lens.data_ptr(), out.slots.data_ptr(),
+                               out.positions.data_ptr(), out.counts.data_ptr())
+        self._check(self._lib.spd_paged_plan(self._h, ctypes.byref(step)))
+        return out
+
+    def paged_append(self, cache: PagedCache, k_new, v_new, slots):
+        """Row t of `k_new` and `v_new` (tokens, heads, head_dim) into the cache's slot slots[t] (int64; -1 drops the row), and
+        the bounds of the pages that get one (spd_paged_append)."""
+        import torch
+        heads, n = cache.k.shape[2], k_new.shape[0]
+        rows = [_rows(x, heads, cache, name) for x, name in ((k_new, "k_new"), (v_new, "v_new"))]
+        if v_new.shape[0] != n or slots.shape != (n,) or slots.dtype != torch.int64 or slots.device != k_new.device or not slots.is_contiguous():
+            raise ValueError("slots must be int64, contiguous, on the cache's device, and as many as rows of k_new and of v_new")
+        self._check(self._lib.spd_paged_append(self._h, cache._ref, n, ctypes.byref(rows[0]), ctypes.byref(rows[1]), slots.data_ptr()))
+
+    def paged_workspace_bytes(self, cache: PagedCache, batch: PagedBatch, n_tokens: int, n_heads: int, n_select: int = 0) -> int:
+        """Scratch of one paged_attention, or with `n_select` paged_sparse_attention, call (spd_paged_workspace_bytes)."""
+        bytes_ = ctypes.c_size_t()
+        batch._struct.n_tokens = int(n_tokens)
+        self._check(self._lib.spd_paged_workspace_bytes(self._h, cache._ref, batch._ref, int(n_heads), int(n_select),
+                                                        ctypes.byref(bytes_)))
+        return int(bytes_.value)
+
+    def paged_attention(self, cache: PagedCache, q, batch: PagedBatch, scale=None, out=None, lse=None):
+        """(out, lse): attention of the new tokens' queries `q` (tokens, heads, head_dim) over their requests' pages, each up to
+        its own position (spd_paged_attention).  `scale` is 1/sqrt(head_dim) unless given."""
+        import torch
+        t, heads, dim = q.shape
+        rows, device = _rows(q, 0, cache, "q"), q.device
+        out = _out(out, (t, heads, dim), q.dtype, device, "out")
+        lse = _out(lse, (t, heads), torch.float32, device, "lse")
+        batch._struct.n_tokens = t
+        self._check(self._lib.spd_paged_attention(self._h, cache._ref, batch._ref, ctypes.byref(rows), heads,
+                                                  dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr()))
+        return out, lse
+
+    def paged_sparse_attention(self, cache: PagedCache, q, batch: PagedBatch, n_select: int, scale=None, out=None, lse=None, selected=None):
+        """(out, lse, selected): the same over `n_select` pages of each token and key head, the request's first, the token's own
+        and those whose bounds score best; selected (tokens, key heads, n_select) are their places in the block table, ascending,
+        then -1 (spd_paged_sparse_attention)."""
+        import torch
+        t, heads, dim = q.shape
+        rows, device = _rows(q, 0, cache, "q"), q.device
+        out = _out(out, (t, heads, dim), q.dtype, device, "out")
+        lse = _out(lse, (t, heads), torch.float32, device, "lse")
+        selected = _out(selected, (t, cache.k.shape[2], max(int(n_select), 0)), torch.int32, device, "selected")
+        batch._struct.n_tokens = t
+        self._check(self._lib.spd_paged_sparse_attention(self._h, cache._ref, batch._ref, ctypes.byref(rows), heads,
+                                                         dim ** -0.5 if scale is None else scale, n_select, selected.data_ptr(),
+                                                         out.data_ptr(), lse.data_ptr()))
+        return out, lse, selected
 
 
 class Index_:

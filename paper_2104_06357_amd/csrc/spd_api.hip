@@ -21,6 +21,7 @@
 #include "spd_direct.h"
 #include "spd_kernels.h"
 #include "spd_match.h"
+#include "spd_paged.h"
 #include "spd_plan.h"
 
 using namespace spd;
@@ -360,12 +361,19 @@ spd_status ensure_workspace(spd_handle *h, size_t bytes) {
     return SPD_OK;
 }
 
+// Profile mode: the events of the call before go back to the pool.
+void forget_timed(spd_handle *h) {
+    for (auto &t : h->timed) { h->event_pool.push_back(t.start); h->event_pool.push_back(t.stop); }
+    h->timed.clear();
+}
+
 // Profile mode: events around one launch.
 struct LaunchTimer {
     spd_handle *h;
     bool on;
     spd_handle::Timed t;
     hipStream_t stream;
+    LaunchTimer(spd_handle *hh, const char *name) : LaunchTimer(hh, name, 0, 0, 0, 0, 0, 0) {}
     LaunchTimer(spd_handle *hh, const char *name, int R, int kind, int block, uint32_t lds, int64_t a_rows, int64_t wgs,
                 hipStream_t st = nullptr)
         : h(hh), on(hh->profile), stream(st ? st : hh->stream) {
@@ -1117,8 +1125,7 @@ spd_status refuse_rows(spd_handle *h, const char *name, const int64_t *ip, int64
 
 spd_status run(spd_handle *h, const spd_csr *A, const spd_csr *B, int metric, float p, const spd_semiring *semiring,
                int knn_k, float *out, int64_t *out_idx, float *out_dist, const spd_index *index = nullptr) {
-    for (auto &t : h->timed) { h->event_pool.push_back(t.start); h->event_pool.push_back(t.stop); }
-    h->timed.clear();
+    forget_timed(h);
     if (A->n_rows == 0 || B->n_rows == 0) return SPD_OK;
     hipError_t e = hipSetDevice(h->device);
     if (e != hipSuccess) return hip_fail(h, e, "hipSetDevice");
@@ -1739,6 +1746,93 @@ size_t workspace_bound(const spd_handle *h, const spd_csr *A, const spd_csr *B, 
     }
     return total;
 }
+// ---- attention over a paged cache ----------------------------------------------------------------
+
+constexpr int64_t kPagedMost = ((int64_t)1 << 31) - 1;        // what the kernels count in 32 bits
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+spd_status check_paged_cache(spd_handle *h, const spd_paged_cache *c) {
+    if (!c) return fail(h, SPD_ERR_NULL, "cache is NULL");
+    if ((int)c->dtype < 0 || (int)c->dtype >= SPD_DTYPE_COUNT) return fail(h, SPD_ERR_UNSUPPORTED, "unknown dtype of the cache");
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0)
+        return fail(h, SPD_ERR_UNSUPPORTED, "page_size must be a power of two from 16 to 1024");
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(h, SPD_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if (c->n_kv_heads < 1 || c->n_pages < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "cache has no heads or a negative size");
+    if (c->n_kv_heads > 65535 || c->n_pages >= kPagedMost) return fail(h, SPD_ERR_UNSUPPORTED, "more than 65535 key heads or 2^31-2 pages");
+    if (c->n_pages > 0 && (!c->k || !c->v)) return fail(h, SPD_ERR_NULL, "k or v of the cache is NULL");
+    if (((c->page_stride | c->token_stride | c->head_stride) & 7) != 0 || !aligned16(c->k) || !aligned16(c->v))
+        return fail(h, SPD_ERR_UNSUPPORTED, "strides of the cache must be multiples of 8 elements, k and v 16-byte aligned");
+    if ((c->bounds != nullptr) != (c->codes != nullptr) || (c->bounds != nullptr) != (c->code_scale != nullptr))
+        return fail(h, SPD_ERR_NULL, "bounds, codes and code_scale of the cache go together");
+    if (!aligned16(c->bounds) || !aligned16(c->codes)) return fail(h, SPD_ERR_UNSUPPORTED, "bounds and codes must be 16-byte aligned");
+    return SPD_OK;
+}
+
+spd_status check_paged_rows(spd_handle *h, const spd_rows *r, const char *name) {
+    if (!r || !r->ptr) return fail(h, SPD_ERR_NULL, std::string(name) + " is NULL");
+    if (((r->token_stride | r->head_stride) & 7) != 0 || !aligned16(r->ptr))
+        return fail(h, SPD_ERR_UNSUPPORTED, std::string("strides of ") + name + " must be multiples of 8 elements, its pointer 16-byte aligned");
+    return SPD_OK;
+}
+
+PagedAttention paged_attention_args(const spd_paged_cache &c, const spd_paged_batch &b, int n_heads) {
+    PagedAttention a{};
+    a.dtype = c.dtype;
+    a.head_dim = c.head_dim;
+    a.cache = PagedCache{c.k, c.v, c.page_stride, c.token_stride, c.head_stride, (int32_t)c.n_pages,
+                         c.page_size > 0 ? __builtin_ctz((unsigned)c.page_size) : 0, c.n_kv_heads, c.codes, c.code_scale};
+    a.req = PagedRequests{b.query_start, b.kv_lens, b.block_table, b.table_stride, (int32_t)b.n_requests, (int32_t)b.n_tokens,
+                          (int32_t)b.max_pages};
+    a.q.heads = n_heads;
+    a.q.group = n_heads / c.n_kv_heads;
+    return a;
+}
+
+spd_status run_paged(spd_handle *h, const spd_paged_cache *c, const spd_paged_batch *b, const spd_rows *q, int n_heads, float scale,
+                     int n_select, int32_t *selected, void *out, float *lse) {
+    if (!h) return SPD_ERR_NULL;
+    h->err.clear();
+    spd_status st = check_paged_cache(h, c);
+    if (st != SPD_OK) return st;
+    if (!b) return fail(h, SPD_ERR_NULL, "batch is NULL");
+    if (b->n_requests < 0 || b->n_tokens < 0 || b->max_pages < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "batch has a negative size");
+    if (n_heads < 1 || n_heads % c->n_kv_heads != 0)
+        return fail(h, SPD_ERR_DIM_MISMATCH, "n_heads must be a multiple of the cache's n_kv_heads");
+    if (b->n_requests >= kPagedMost || b->n_tokens * (int64_t)n_heads >= kPagedMost || b->n_tokens >= kPagedMost || n_heads > 65535 ||
+        b->max_pages * (int64_t)c->page_size >= kPagedMost)
+        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 requests, rows of queries (tokens x heads) or tokens of a request");
+    if (b->n_requests > 1 && b->table_stride < b->max_pages)
+        return fail(h, SPD_ERR_DIM_MISMATCH, "rows of block_table overlap (table_stride < max_pages)");
+    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(h, SPD_ERR_UNSUPPORTED, "scale must be finite and positive");
+    if (n_select > 0 && !c->codes) return fail(h, SPD_ERR_NULL, "the cache has no bounds to select pages by");
+    if (b->n_tokens == 0 || b->n_requests == 0) return SPD_OK;
+    if (!b->query_start || !b->kv_lens || (b->max_pages > 0 && !b->block_table)) return fail(h, SPD_ERR_NULL, "batch has a NULL array");
+    if ((st = check_paged_rows(h, q, "q")) != SPD_OK) return st;
+    if (!out || !aligned16(out)) return fail(h, out ? SPD_ERR_UNSUPPORTED : SPD_ERR_NULL, "out is NULL or not 16-byte aligned");
+    if (n_select > 0 && !selected) return fail(h, SPD_ERR_NULL, "selected is NULL");
+    PagedAttention a = paged_attention_args(*c, *b, n_heads);
+    a.q.ptr = q->ptr;
+    a.q.token_stride = q->token_stride;
+    a.q.head_stride = q->head_stride;
+    a.q.scale = scale * 1.4426950408889634f;
+    a.out = PagedOut{out, lse};
+    a.selected = selected;
+    a.n_select = n_select;
+    const size_t for_select = n_select > 0 ? align256(paged_select_scratch(a)) : 0;
+    if ((st = ensure_workspace(h, for_select + paged_attention_scratch(a, h->opt.n_cus))) != SPD_OK) return st;
+    forget_timed(h);
+    if (n_select > 0) {
+        LaunchTimer timer(h, "paged_select");
+        const hipError_t e = launch_paged_select(h->stream, a, selected, h->ws);
+        timer.done();
+        if (e != hipSuccess) return hip_fail(h, e, "paged selection kernel");
+    }
+    LaunchTimer timer(h, "paged_attention");
+    const hipError_t e = launch_paged_attention(h->stream, a, static_cast<unsigned char *>(h->ws) + for_select, h->opt.n_cus);
+    timer.done();
+    return e == hipSuccess ? SPD_OK : hip_fail(h, e, "paged attention kernel");
+}
 }  // namespace
 
 extern "C" {
@@ -1826,8 +1920,7 @@ spd_status spd_index_create(spd_handle *h, const spd_csr *Index, spd_metric metr
     if (st != SPD_OK) return st;
     if ((int)metric < 0 || (int)metric >= SPD_METRIC_COUNT) return fail(h, SPD_ERR_BAD_METRIC, "unknown metric");
     if (metric == SPD_MINKOWSKI && !(p > 0.0f && std::isfinite(p))) return fail(h, SPD_ERR_BAD_P, "Minkowski needs a finite p > 0");
-    for (auto &t : h->timed) { h->event_pool.push_back(t.start); h->event_pool.push_back(t.stop); }
-    h->timed.clear();
+    forget_timed(h);
     hipError_t e = hipSetDevice(h->device);
     if (e != hipSuccess) return hip_fail(h, e, "hipSetDevice");
     const int64_t n = Index->n_rows;
@@ -1928,6 +2021,75 @@ spd_status spd_index_knn(spd_handle *h, const spd_csr *Q, const spd_index *index
     if (st != SPD_OK) return st;
     if (index->device != h->device) return fail(h, SPD_ERR_UNSUPPORTED, "the index lives on another device");
     return run(h, Q, &index->matrix, index->metric, index->p, nullptr, k, nullptr, out_idx, out_dist, index);
+}
+
+spd_status spd_paged_plan(spd_handle *h, const spd_paged_step *s) {
+    if (!h) return SPD_ERR_NULL;
+    h->err.clear();
+    if (!s) return fail(h, SPD_ERR_NULL, "step is NULL");
+    if (s->n_requests < 0 || s->n_tokens < 0 || s->max_pages < 0 || s->n_free < 0)
+        return fail(h, SPD_ERR_DIM_MISMATCH, "step has a negative size");
+    if (s->page_size < 16 || s->page_size > 1024 || (s->page_size & (s->page_size - 1)) != 0)
+        return fail(h, SPD_ERR_UNSUPPORTED, "page_size must be a power of two from 16 to 1024");
+    if (s->n_requests > SPD_PAGED_MAX_REQUESTS)
+        return fail(h, SPD_ERR_UNSUPPORTED, "more than " + std::to_string(SPD_PAGED_MAX_REQUESTS) + " requests");
+    if (s->n_tokens >= kPagedMost || s->max_pages >= kPagedMost || s->n_free >= kPagedMost)
+        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 tokens, pages of a request or free pages");
+    if (s->n_requests > 1 && s->table_stride < s->max_pages)
+        return fail(h, SPD_ERR_DIM_MISMATCH, "rows of block_table overlap (table_stride < max_pages)");
+    if (!s->query_start || !s->counts || (s->n_requests > 0 && (!s->past_lens || !s->new_lens || !s->kv_lens)) ||
+        (s->n_requests > 0 && s->max_pages > 0 && !s->block_table) || (s->n_free > 0 && !s->free_pages) ||
+        (s->n_tokens > 0 && (!s->slots || !s->positions)))
+        return fail(h, SPD_ERR_NULL, "step has a NULL array");
+    forget_timed(h);
+    LaunchTimer timer(h, "paged_plan");
+    const hipError_t e = launch_paged_plan(h->stream, *s);
+    timer.done();
+    return e == hipSuccess ? SPD_OK : hip_fail(h, e, "paged plan kernel");
+}
+
+spd_status spd_paged_append(spd_handle *h, const spd_paged_cache *c, int64_t n_tokens, const spd_rows *k_new, const spd_rows *v_new,
+                            const int64_t *slots) {
+    if (!h) return SPD_ERR_NULL;
+    h->err.clear();
+    spd_status st = check_paged_cache(h, c);
+    if (st != SPD_OK) return st;
+    if (n_tokens < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "negative number of tokens");
+    if (n_tokens >= kPagedMost) return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 tokens");
+    if (n_tokens == 0) return SPD_OK;
+    if (!slots) return fail(h, SPD_ERR_NULL, "slots is NULL");
+    if ((st = check_paged_rows(h, k_new, "k_new")) != SPD_OK || (st = check_paged_rows(h, v_new, "v_new")) != SPD_OK) return st;
+    forget_timed(h);
+    LaunchTimer timer(h, "paged_append");
+    const hipError_t e = launch_paged_append(h->stream, *c, n_tokens, *k_new, *v_new, slots);
+    timer.done();
+    return e == hipSuccess ? SPD_OK : hip_fail(h, e, "paged append kernel");
+}
+
+spd_status spd_paged_workspace_bytes(const spd_handle *h, const spd_paged_cache *c, const spd_paged_batch *b, int n_heads, int n_select,
+                                     size_t *bytes) {
+    if (!h || !c || !b || !bytes) return SPD_ERR_NULL;
+    if (c->n_kv_heads < 1 || n_heads < 1 || n_heads % c->n_kv_heads != 0 || b->n_requests < 0 || b->n_tokens < 0 || b->max_pages < 0)
+        return SPD_ERR_DIM_MISMATCH;
+    PagedAttention a = paged_attention_args(*c, *b, n_heads);
+    a.n_select = n_select;
+    a.selected = n_select > 0 ? reinterpret_cast<const int32_t *>(bytes) : nullptr;      // (only looked at for being there)
+    *bytes = align256(paged_attention_scratch(a, h->opt.n_cus)) + (n_select > 0 ? align256(paged_select_scratch(a)) : 0);
+    return SPD_OK;
+}
+
+spd_status spd_paged_attention(spd_handle *h, const spd_paged_cache *c, const spd_paged_batch *b, const spd_rows *q, int n_heads, float scale,
+                               void *out, float *lse) {
+    return run_paged(h, c, b, q, n_heads, scale, 0, nullptr, out, lse);
+}
+
+spd_status spd_paged_sparse_attention(spd_handle *h, const spd_paged_cache *c, const spd_paged_batch *b, const spd_rows *q, int n_heads,
+                                      float scale, int n_select, int32_t *selected, void *out, float *lse) {
+    if (!h) return SPD_ERR_NULL;
+    h->err.clear();
+    if (n_select < 2 || n_select > SPD_PAGED_MAX_SELECT)
+        return fail(h, SPD_ERR_BAD_K, "n_select must lie in 2 .. " + std::to_string(SPD_PAGED_MAX_SELECT));
+    return run_paged(h, c, b, q, n_heads, scale, n_select, selected, out, lse);
 }
 
 spd_status spd_csr_validate(spd_handle *h, const spd_csr *M, int require_nonnegative) {

@@ -1,0 +1,56 @@
+// Attention over a paged cache and the calls around it (include/spd.h): what the kernels are given.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/spd.h"
+
+namespace spd {
+
+struct PagedCache {
+    const void *k, *v;
+    int64_t page_stride, token_stride, head_stride;     // elements
+    int32_t n_pages, page_shift, kv_heads;
+    const int8_t *codes;
+    const float *code_scale;
+};
+
+struct PagedRequests {
+    const int32_t *query_start, *kv_lens, *block_table;
+    int64_t table_stride;
+    int32_t n_requests, n_tokens, max_pages;
+};
+
+struct PagedQueries {
+    const void *ptr;
+    int64_t token_stride, head_stride;
+    int32_t heads, group;                               // group: query heads to a key head
+    float scale;                                        // of the logits, times log2(e)
+};
+
+struct PagedOut { void *out; float *lse; };
+
+constexpr int kPagedWave = 64;
+
+hipError_t launch_paged_plan(hipStream_t st, const spd_paged_step &s);
+hipError_t launch_paged_append(hipStream_t st, const spd_paged_cache &c, int64_t n_tokens, const spd_rows &k_new,
+                               const spd_rows &v_new, const int64_t *slots);
+
+// Attention of the chunk; with `selected`, over the pages it lists (n_select to a token and key head).
+struct PagedAttention {
+    spd_dtype dtype;
+    int32_t head_dim;
+    PagedCache cache;
+    PagedRequests req;
+    PagedQueries q;
+    PagedOut out;
+    const int32_t *selected;
+    int32_t n_select;
+};
+size_t paged_attention_scratch(const PagedAttention &a, int n_cus);
+hipError_t launch_paged_attention(hipStream_t st, const PagedAttention &a, void *scratch, int n_cus);
+
+size_t paged_select_scratch(const PagedAttention &a);
+hipError_t launch_paged_select(hipStream_t st, const PagedAttention &a, int32_t *selected, void *scratch);
+
+}  // namespace spd

@@ -1,0 +1,254 @@
+// Block tables, slots and positions of a step's new tokens, and the append of their keys and values.
+#include <algorithm>
+
+#include "spd_paged_device.h"
+
+namespace spd {
+
+namespace {
+
+constexpr int kPlanThreads = 1024;
+
+// First of the `n` ascending numbers behind `s` that is greater than x, less one: s[i] <= x < s[i + 1].
+__device__ __forceinline__ int last_at_most(const int32_t *s, int n, int32_t x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ int32_t saturated(int64_t v) { return (int32_t)min(v, (int64_t)INT32_MAX); }
+
+// The requests' first tokens and first fresh pages are two prefix sums.  Every workgroup makes both for itself (16,384
+// requests are two 64 KB arrays of LDS), which costs it the reading of 8 bytes a request out of L2, and then numbers its share of
+// the tokens and of the pages: one launch, no workgroup waits for another.  Bound by the launch and the scan's latency: the
+// outputs are 12 bytes a token.
+__global__ void __launch_bounds__(kPlanThreads) spd_paged_plan_kernel(const spd_paged_step s, const int shift) {
+    extern __shared__ int32_t s_first[];                          // tokens, then pages: n_requests + 1 of each
+    __shared__ int64_t s_wave[kPlanThreads / 64][2];
+    const int n = (int)s.n_requests, tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int32_t *const s_tokens = s_first, *const s_pages = s_first + n + 1;
+    const int64_t page = (int64_t)1 << shift;
+    int64_t tokens = 0, pages = 0;                                // of the requests before this round's
+    for (int base = 0; base < n; base += kPlanThreads) {
+        const int r = base + tid;
+        int64_t a = 0, b = 0;
+        if (r < n) {
+            const int64_t past = max(s.past_lens[r], 0), fresh = max(s.new_lens[r], 0);
+            a = fresh;
+            b = min((past + fresh + page - 1) >> shift, s.max_pages) - min((past + page - 1) >> shift, s.max_pages);
+        }
+        int64_t ia = a, ib = b;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t ua = __shfl_up(ia, d), ub = __shfl_up(ib, d);
+            if (lane >= d) { ia += ua; ib += ub; }
+        }
+        if (lane == 63) { s_wave[wave][0] = ia; s_wave[wave][1] = ib; }
+        __syncthreads();
+        int64_t ta = 0, tb = 0;
+#pragma unroll
+        for (int w = 0; w < kPlanThreads / 64; ++w) {
+            if (w < wave) { ia += s_wave[w][0]; ib += s_wave[w][1]; }
+            ta += s_wave[w][0]; tb += s_wave[w][1];
+        }
+        if (r < n) { s_tokens[r] = saturated(tokens + ia - a); s_pages[r] = saturated(pages + ib - b); }
+        tokens += ta; pages += tb;
+        __syncthreads();
+    }
+    if (tid == 0) { s_tokens[n] = saturated(tokens); s_pages[n] = saturated(pages); }
+    __syncthreads();
+    const int64_t at = (int64_t)blockIdx.x * kPlanThreads + tid, step = (int64_t)gridDim.x * kPlanThreads;
+    for (int64_t r = at; r <= n; r += step) {
+        s.query_start[r] = s_tokens[r];
+        if (r < n) s.kv_lens[r] = saturated((int64_t)max(s.past_lens[r], 0) + max(s.new_lens[r], 0));
+    }
+    if (at == 0) {
+        s.counts[0] = s_tokens[n];
+        s.counts[1] = (int32_t)min(pages, s.n_free);
+        s.counts[2] = saturated(pages - min(pages, s.n_free));
+    }
+    // (an entry's rank among the fresh ones is its number in free_pages)
+    for (int64_t g = at; g < s_pages[n]; g += step) {
+        const int r = last_at_most(s_pages, n, (int32_t)g);
+        const int64_t col = (((int64_t)max(s.past_lens[r], 0) + page - 1) >> shift) + g - s_pages[r];
+        s.block_table[r * s.table_stride + col] = g < s.n_free ? s.free_pages[g] : -1;
+    }
+    for (int64_t t = at; t < s.n_tokens; t += step) {
+        int64_t slot = -1;
+        int32_t position = -1;
+        if (t < s_tokens[n]) {
+            const int r = last_at_most(s_tokens, n, (int32_t)t);
+            const int64_t past = max(s.past_lens[r], 0), p = past + t - s_tokens[r], col = p >> shift, have = (past + page - 1) >> shift;
+            position = (int32_t)p;
+            int32_t number = -1;
+            if (col < s.max_pages) {
+                if (col < have) number = s.block_table[r * s.table_stride + col];
+                else if (const int64_t g = s_pages[r] + col - have; g < s.n_free) number = s.free_pages[g];
+            }
+            if (number >= 0) slot = ((int64_t)number << shift) + (p & (page - 1));
+        }
+        s.slots[t] = slot;
+        s.positions[t] = position;
+    }
+}
+
+constexpr int kAppendRows = 16;                                   // rows of a workgroup's window
+
+struct AppendArgs {
+    spd_paged_cache c;
+    int64_t n_tokens;
+    spd_rows k_new, v_new;
+    const int64_t *slots;
+    int32_t shift;
+};
+
+// Whether row t goes on in the page that row t - 1 is in, at the next slot.
+__device__ __forceinline__ bool goes_on(const AppendArgs &a, int64_t t, int64_t slot) {
+    return t > 0 && (slot & (((int64_t)1 << a.shift) - 1)) != 0 && a.slots[t - 1] == slot - 1;
+}
+
+// A workgroup has one key head and a window of 16 rows, D/8 lanes to a row, 16 bytes to a lane.  It moves the runs (rows of
+// one page, slots one after the other) that begin in its window, to their ends: at most one of them, the window's last, goes past it, and is
+// taken by all lanes together.  So every bound has one writer, which has seen all of its keys, and no row is read twice.
+template <spd_dtype T, int D>
+__global__ void __launch_bounds__(kAppendRows * D / 8) spd_paged_append_kernel(const AppendArgs a) {
+    using H = half_t<T>;
+    using H8 = half8_t<T>;
+    constexpr int kLanes = D / 8;
+    __shared__ int64_t s_slot[kAppendRows];
+    __shared__ int32_t s_run[kAppendRows];                        // the row of the window at which the row's run begins; -1: before the window, or no slot
+    __shared__ __align__(16) float s_lo[2][kAppendRows][D], s_hi[2][kAppendRows][D];      // of the window's rows, and of those past it
+    __shared__ int32_t s_past;                                    // rows past the window that its last run has
+    const int tid = (int)threadIdx.x, row = tid / kLanes, part = tid % kLanes, head = (int)blockIdx.y;
+    const int64_t t0 = (int64_t)blockIdx.x * kAppendRows, page = (int64_t)1 << a.shift, most = a.c.n_pages << a.shift;
+    if (tid < 64) {                                               // the first wavefront: a row to a lane, the window's and those after it
+        int64_t t = t0 + tid, slot = t < a.n_tokens ? a.slots[t] : -1;
+        const bool real = slot >= 0 && slot < most;
+        uint64_t on = __ballot(real && goes_on(a, t, slot));
+        if (tid < kAppendRows) {
+            // (a row that does not go on begins a run; one that does belongs to the nearest of those before it)
+            const uint64_t begins = ~on & ((2ull << tid) - 1);
+            s_slot[tid] = slot;
+            s_run[tid] = real && begins ? 63 - __builtin_clzll(begins) : -1;
+        }
+        int past = 0;
+        if ((~on & ((1ull << kAppendRows) - 1)) != 0) {           // (else the whole window belongs to a run from before it)
+            on >>= kAppendRows;
+            int looked = 64 - kAppendRows;
+            for (;;) {
+                const int more = on == ~0ull ? 64 : __builtin_ctzll(~on);
+                past += min(more, looked);
+                if (more < looked) break;
+                t = t0 + kAppendRows + past + tid;
+                slot = t < a.n_tokens ? a.slots[t] : -1;
+                on = __ballot(slot >= 0 && slot < most && goes_on(a, t, slot));
+                looked = 64;
+            }
+        }
+        if (tid == 0) s_past = past;
+    }
+    __syncthreads();
+    const int64_t cache_at = (int64_t)head * a.c.head_stride + part * 8;
+    const H *const k_new = (const H *)a.k_new.ptr + head * a.k_new.head_stride + part * 8;
+    const H *const v_new = (const H *)a.v_new.ptr + head * a.v_new.head_stride + part * 8;
+    float lo[8], hi[8];
+    auto move = [&](int64_t t, int64_t slot) {
+        const H8 k = *(const H8 *)(k_new + t * a.k_new.token_stride), v = *(const H8 *)(v_new + t * a.v_new.token_stride);
+        const int64_t to = (slot >> a.shift) * a.c.page_stride + (slot & (page - 1)) * a.c.token_stride + cache_at;
+        *(H8 *)((H *)a.c.k + to) = k;
+        *(H8 *)((H *)a.c.v + to) = v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], (float)k[e]); hi[e] = fmaxf(hi[e], (float)k[e]); }
+    };
+    auto keep = [&](int which) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { s_lo[which][row][part * 8 + e] = lo[e]; s_hi[which][row][part * 8 + e] = hi[e]; }
+    };
+    auto forget = [&] {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { lo[e] = __builtin_inff(); hi[e] = -__builtin_inff(); }
+    };
+    auto join = [&](int which, int i) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], s_lo[which][i][part * 8 + e]); hi[e] = fmaxf(hi[e], s_hi[which][i][part * 8 + e]); }
+    };
+    const int run = s_run[row], last = s_run[kAppendRows - 1], past = s_past;
+    forget();
+    if (run >= 0) move(t0 + row, s_slot[row]);
+    keep(0);
+    if (past > 0) {                                               // all rows' lanes together
+        forget();
+        for (int i = row; i < past; i += kAppendRows) move(t0 + kAppendRows + i, s_slot[kAppendRows - 1] + 1 + i);
+        keep(1);
+    }
+    if (a.c.bounds == nullptr) return;
+    __syncthreads();
+    if (run != row) return;                                       // the first row of a run writes its bounds
+    forget();
+    for (int i = row; i < kAppendRows && s_run[i] == run; ++i) join(0, i);
+    if (past > 0 && run == last) for (int i = 0; i < kAppendRows; ++i) join(1, i);
+    const int64_t slot = s_slot[row], at = ((slot >> a.shift) * a.c.n_kv_heads + head) * 2 * D + part * 8;
+    H *const kept = (H *)a.c.bounds + at;
+    H8 l, h;
+    if ((slot & (page - 1)) != 0) {
+        l = *(const H8 *)kept;
+        h = *(const H8 *)(kept + D);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], (float)l[e]); hi[e] = fmaxf(hi[e], (float)h[e]); }
+    }
+    float big = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { l[e] = (H)lo[e]; h[e] = (H)hi[e]; big = fmaxf(big, fmaxf(fabsf(lo[e]), fabsf(hi[e]))); }
+    *(H8 *)kept = l;
+    *(H8 *)(kept + D) = h;
+#pragma unroll
+    for (int d = 1; d < kLanes; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
+    const float scale = big * kPagedCodeStep;
+    union { int8_t b[8]; uint64_t w; } cl, ch;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        cl.b[e] = (int8_t)(scale > 0.0f ? (int)rintf(lo[e] / scale) : 0);
+        ch.b[e] = (int8_t)(scale > 0.0f ? (int)rintf(hi[e] / scale) : 0);
+    }
+    *(uint64_t *)(a.c.codes + at) = cl.w;
+    *(uint64_t *)(a.c.codes + at + D) = ch.w;
+    if (part == 0) a.c.code_scale[(slot >> a.shift) * a.c.n_kv_heads + head] = scale;
+}
+
+}  // namespace
+
+hipError_t launch_paged_plan(hipStream_t st, const spd_paged_step &s) {
+    const int shift = __builtin_ctz((unsigned)s.page_size);
+    const size_t lds = (size_t)(s.n_requests + 1) * 8;
+    // tokens and requests are each dealt to enough workgroups; more of them would only repeat the scan
+    const int64_t most = std::max<int64_t>(s.n_tokens, s.n_requests + 1);
+    const int64_t groups = std::min<int64_t>((most + kPlanThreads - 1) / kPlanThreads, 256);
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(spd_paged_plan_kernel),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(spd_paged_plan_kernel, dim3((unsigned)std::max<int64_t>(groups, 1)), dim3(kPlanThreads), lds, st, s, shift);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_append(hipStream_t st, const spd_paged_cache &c, int64_t n_tokens, const spd_rows &k_new,
+                               const spd_rows &v_new, const int64_t *slots) {
+    if (n_tokens == 0) return hipSuccess;
+    AppendArgs a{c, n_tokens, k_new, v_new, slots, __builtin_ctz((unsigned)c.page_size)};
+    const dim3 grid((unsigned)((n_tokens + kAppendRows - 1) / kAppendRows), (unsigned)c.n_kv_heads);
+    const dim3 block((unsigned)(kAppendRows * c.head_dim / 8));
+    if (c.dtype == SPD_BF16) {
+        if (c.head_dim == 64) hipLaunchKernelGGL((spd_paged_append_kernel<SPD_BF16, 64>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((spd_paged_append_kernel<SPD_BF16, 128>), grid, block, 0, st, a);
+    } else {
+        if (c.head_dim == 64) hipLaunchKernelGGL((spd_paged_append_kernel<SPD_F16, 64>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((spd_paged_append_kernel<SPD_F16, 128>), grid, block, 0, st, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace spd

@@ -1,0 +1,539 @@
+"""Attention over a paged cache and the calls around it against their definitions in 64 bits (tests/paged_reference.py), where
+pages, tiles, runs and groups of heads end, and the calls' refusals (needs an MI355X; run with -m gpu)."""
+import numpy as np
+import pytest
+import torch
+
+from paged_reference import DTYPES, World, assert_close, pages_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def spd():
+    import paper_2104_06357_amd as lib
+    return lib
+
+
+@pytest.fixture(scope="module")
+def h(spd):
+    handle = spd.Handle()
+    yield handle
+    handle.close()
+
+
+# ------------------------------------------------------------------------------------------------ plan
+
+def plan_by_hand(past, new, free, table, page, n_tokens):
+    """The definition, token by token."""
+    table = table.copy()
+    width = table.shape[1]
+    starts, slots, positions = [0], np.full(n_tokens, -1, np.int64), np.full(n_tokens, -1, np.int32)
+    taken = missing = 0
+    for r, (p, m) in enumerate(zip(past, new)):
+        p, m = max(p, 0), max(m, 0)
+        for j in range(min(pages_of(p, page), width), min(pages_of(p + m, page), width)):
+            table[r, j] = free[taken] if taken < len(free) else -1
+            taken, missing = taken + (taken < len(free)), missing + (taken >= len(free))
+        for i in range(m):
+            t = starts[-1] + i
+            if t < n_tokens:
+                positions[t] = p + i
+                j = (p + i) // page
+                if j < width and table[r, j] >= 0:
+                    slots[t] = int(table[r, j]) * page + (p + i) % page
+        starts.append(starts[-1] + m)
+    return table, starts, [max(p, 0) + max(m, 0) for p, m in zip(past, new)], slots, positions, [starts[-1], taken, missing]
+
+
+def check_plan(spd, h, past, new, free, table, page, n_tokens, out=None):
+    want = plan_by_hand(past, new, free, table, page, n_tokens)
+    i32 = lambda v: torch.from_numpy(np.asarray(v, dtype=np.int32)).cuda()  # noqa: E731
+    dev = i32(table)
+    b = h.paged_plan(i32(past), i32(new), i32(free), dev, page, n_tokens, out=out)
+    torch.cuda.synchronize()
+    got = [x.cpu().numpy() for x in (dev, b.query_start, b.kv_lens, b.slots, b.positions)]
+    # (a page is counted as missing once it has been wanted and the free ones are out)
+    counts = b.counts.cpu().tolist()
+    for name, x, y in zip(("table", "query_start", "kv_lens", "slots", "positions"), got, want):
+        assert np.array_equal(x, np.asarray(y)), name
+    assert counts[0] == want[5][0] and counts[1] == want[5][1]
+    return counts[2]
+
+
+@pytest.mark.parametrize("page", [16, 64, 1024])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 1000, 1024, 1025, 3000])
+def test_plan(spd, h, n, page):
+    rng = np.random.default_rng(n + page)
+    past = rng.integers(0, 5 * page, n)
+    new = np.where(rng.random(n) < 0.5, 1, rng.integers(0, 3 * page if n < 500 else 40, n))
+    past[0], new[-1] = page, page                       # ends of pages
+    width = int(pages_of(past + new, page).max()) + 1
+    pages = rng.permutation(n * width).astype(np.int32)
+    have = pages_of(past, page)
+    table = np.full((n, width), -1, np.int32)
+    at = 0
+    for r in range(n):
+        table[r, :have[r]] = pages[at:at + have[r]]
+        at += have[r]
+    print("plan", n, page, flush=True)
+    total = int(new.sum())
+    assert check_plan(spd, h, past, new, pages[at:], table, page, total) == 0
+    check_plan(spd, h, past, new, pages[at:], table, page, total + 77)       # more places than tokens
+    check_plan(spd, h, past, new, pages[at:], table, page, total // 2)       # fewer
+
+
+def test_plan_runs_out_of_pages_and_of_columns(spd, h):
+    table = np.arange(12, dtype=np.int32).reshape(3, 4)
+    past, new = [40, 16, 0], [40, 100, 5]
+    assert check_plan(spd, h, past, new, [100, 101], table, 16, 145) == 3 and check_plan(spd, h, past, new, [], table, 16, 145) == 5
+    check_plan(spd, h, [-5, 3, 0], [2, -7, 0], [100, 101, 102], table, 16, 2)       # negative lengths count as 0
+    check_plan(spd, h, [1000], [5], [7, 8], table[:1], 16, 5)                # a request longer than its table
+
+
+def test_plan_of_nothing_and_of_very_many(spd, h):
+    check_plan(spd, h, [], [], [1], np.zeros((0, 4), np.int32), 16, 3)
+    rng = np.random.default_rng(5)
+    n = 16384
+    past, new = rng.integers(0, 60, n), rng.integers(0, 4, n)
+    table = rng.integers(0, 99, (n, 4)).astype(np.int32)
+    check_plan(spd, h, past, new, np.arange(5000, 5000 + n), table, 16, int(new.sum()))
+
+
+def test_plan_writes_an_earlier_steps_tensors_again(spd, h):
+    table = np.full((2, 4), -1, np.int32)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    dev, free = i32(table.tolist()), i32([5, 6, 7, 8])
+    b = h.paged_plan(i32([0, 0]), i32([3, 2]), free, dev, 16, 5)
+    c = h.paged_plan(i32([3, 2]), i32([2, 3]), free, dev, 16, 5, out=b)
+    assert c is b and b.slots.tolist() == [83, 84, 98, 99, 100] and b.kv_lens.tolist() == [5, 5]
+    with pytest.raises(ValueError):
+        h.paged_plan(i32([3, 2]), i32([2, 3]), free, dev, 16, 6, out=b)
+
+
+# ------------------------------------------------------------------------------------------------ append
+
+def check_append(spd, h, w, chunks, dtype):
+    """`chunks`: lists of (request, tokens) appended one after the other to an empty cache; the end must be the definition's."""
+    dt = DTYPES[dtype]
+    empty = torch.full_like(w.k, 7.0)
+    at = {"thd": lambda x: x.cuda(), "htd": lambda x: x.transpose(1, 2).contiguous().cuda().transpose(1, 2)}[w.layout]
+    cache = spd.PagedCache(at(empty), at(empty), bounds=True)
+    done = [0] * len(w.requests)
+    for chunk in chunks:
+        slots, rows_k, rows_v = [], [], []
+        for r, m in chunk:
+            for p in range(done[r], done[r] + m):
+                number = int(w.table[r, p // w.page])
+                slots.append(number * w.page + p % w.page)
+                rows_k.append(w.k[number, p % w.page])
+                rows_v.append(w.v[number, p % w.page])
+            done[r] += m
+        if not slots:
+            continue
+        both = torch.stack((torch.stack(rows_k), torch.stack(rows_v)), 1).cuda()        # one projection's output: strided rows
+        h.paged_append(cache, both[:, 0], both[:, 1], torch.tensor(slots, device="cuda"))
+    torch.cuda.synchronize()
+    real = torch.zeros(w.k.shape[:2], dtype=torch.bool)
+    for r in range(len(w.requests)):
+        for p in range(done[r]):
+            real[int(w.table[r, p // w.page]), p % w.page] = True
+    for mine, theirs in ((cache.k, w.k), (cache.v, w.v)):
+        mine = mine.cpu()
+        assert torch.equal(mine[real], theirs[real]) and bool((mine[~real] == 7.0).all())
+    w.count = real.sum(1)
+    w.make_bounds()
+    assert torch.equal(cache.bounds.cpu(), w.bounds.to(dt))
+    assert torch.equal(cache.codes.cpu(), w.codes) and torch.equal(cache.code_scale.cpu(), w.code_scale)
+
+
+@pytest.mark.parametrize("dtype,dim,layout", [("bf16", 128, "thd"), ("f16", 64, "htd"), ("bf16", 64, "thd"), ("f16", 128, "htd")])
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_append_in_steps_of_any_size(spd, h, dtype, dim, layout, page):
+    w = World([(0, 3 * page + 5), (0, page), (0, 1), (0, 0), (0, 700)], dtype=dtype, dim=dim, page=page, layout=layout, kv_heads=3, seed=page)
+    print("append", dtype, dim, layout, page, flush=True)
+    check_append(spd, h, w, [[(0, 5), (1, page - 1), (4, 33)], [(0, page), (1, 1), (2, 1)], [(0, 1), (4, 1)], [(0, 2 * page - 1), (4, 666)]], dtype)
+    check_append(spd, h, w, [[(r, n) for r, (_, n) in enumerate(w.requests)]], dtype)
+
+
+def test_append_token_by_token(spd, h):
+    w = World([(0, 40), (0, 21)], page=16, seed=4)
+    check_append(spd, h, w, [[(0, 1), (1, 1 if i < 21 else 0)] for i in range(40)], "bf16")
+
+
+def test_append_drops_rows_without_a_slot(spd, h):
+    w = World([(0, 40)], page=16, kv_heads=1, spare=0, stale=0.0)
+    cache = spd.PagedCache(torch.zeros_like(w.k).cuda(), torch.zeros_like(w.v).cuda(), bounds=True)
+    new = torch.randn((40, 1, 128)).to(torch.bfloat16)
+    slots = torch.arange(40)
+    slots[[3, 17, 39]] = torch.tensor([-1, 3 * 16, 1 << 40])              # no page, past the cache, far past it
+    h.paged_append(cache, new.cuda(), new.cuda(), slots.cuda())
+    got = cache.k.cpu().reshape(48, 1, 128)
+    keep = torch.tensor([i for i in range(40) if i not in (3, 17, 39)])
+    assert torch.equal(got[keep], new[keep]) and not bool(got[[3, 17, 39, 40, 47]].any())
+    assert not bool(torch.isnan(cache.code_scale).any())
+
+
+def test_append_without_bounds_and_of_nothing(spd, h):
+    k = torch.zeros((4, 16, 2, 64), dtype=torch.float16, device="cuda")
+    cache = spd.PagedCache(k, torch.zeros_like(k))
+    new = torch.randn((9, 2, 64), dtype=torch.float16, device="cuda")
+    h.paged_append(cache, new, new, torch.arange(20, 29, device="cuda"))
+    assert torch.equal(k.reshape(64, 2, 64)[20:29], new) and float(k.reshape(64, 2, 64)[:20].abs().max()) == 0
+    h.paged_append(cache, new[:0], new[:0], torch.arange(0, device="cuda"))
+
+
+# ------------------------------------------------------------------------------------------------ attention
+
+def run_chunk(spd, h, w, scale=None):
+    return h.paged_attention(w.cache(spd), w.queries(), w.batch(spd), scale=scale)
+
+
+# around the 16, 32, 64 and 128 rows and keys that tiles have; no tokens, one, whole pages; a chunk longer than its past
+SHAPES = {
+    "one token": [(0, 1)],
+    "decode": [(0, 1), (15, 1), (16, 1), (63, 1), (64, 1), (127, 1), (128, 1), (500, 1), (1023, 1)],
+    "prompt": [(0, 200)],
+    "chunks": [(5, 3), (0, 16), (31, 33), (0, 0), (100, 31), (64, 64), (7, 129)],
+    "long past": [(3000, 2), (1500, 40)],
+}
+
+
+@pytest.mark.parametrize("group", [1, 3, 4, 16, 20])
+@pytest.mark.parametrize("shape", list(SHAPES))
+def test_attention(spd, h, shape, group):
+    requests = SHAPES[shape]
+    heads = 2 if sum(n for _, n in requests) * group < 1500 else 1
+    w = World(requests, group=group, kv_heads=heads, fused=group == 4, seed=group)
+    print("attention", shape, group, flush=True)
+    assert_close(w, run_chunk(spd, h, w), w.attention(), shape)
+
+
+@pytest.mark.parametrize("dtype,dim,layout,page", [("bf16", 64, "htd", 16), ("f16", 128, "thd", 32), ("f16", 64, "thd", 128),
+                                                   ("bf16", 128, "htd", 64), ("f16", 128, "htd", 1024)])
+@pytest.mark.parametrize("shape", ["decode", "chunks"])
+def test_attention_types_and_layouts(spd, h, shape, dtype, dim, layout, page):
+    w = World(SHAPES[shape], dtype=dtype, dim=dim, layout=layout, page=page, fused=True, seed=page)
+    print("attention", shape, dtype, dim, layout, page, flush=True)
+    assert_close(w, run_chunk(spd, h, w, scale=0.2), w.attention(scale=0.2), shape)
+
+
+def test_attention_rows_that_see_nothing(spd, h):
+    """Fewer cached tokens than new ones: the first rows stand before the request begins.  Pages that are not there mask theirs; a length
+    past the table is cut; tokens outside every request are left alone."""
+    w = World([(0, 50), (200, 9), (40, 4), (64, 20)], group=3, seed=8)
+    w.kv_lens[0] = 20                                                      # 30 rows see nothing
+    w.table[1, 3], w.table[1, 7], w.table[1, 12] = -1, w.pages, 2 ** 31 - 1
+    w.table[2] = -1                                                        # nothing of it is there
+    w.kv_lens[3] = 10 ** 6
+    want = w.attention()
+    assert bool(torch.isinf(want[1]).any()) and not bool(torch.isinf(want[1]).all())
+    w.v = torch.nan_to_num(w.v)                                            # (the cut request reaches what was stale)
+    w.k = torch.nan_to_num(w.k)
+    want = w.attention()
+    assert_close(w, run_chunk(spd, h, w), want, "rows that see nothing")
+    cache, batch, q = w.cache(spd), w.batch(spd), w.queries()
+    more = torch.cat((q, q[:5]))
+    out = torch.full(tuple(more.shape), 3.0, dtype=q.dtype, device="cuda")
+    lse = torch.full(tuple(more.shape[:2]), 3.0, device="cuda")
+    h.paged_attention(cache, more, batch, out=out, lse=lse)
+    assert bool((out[-5:] == 3.0).all()) and bool((lse[-5:] == 3.0).all())
+    assert_close(w, (out[:-5], lse[:-5]), want, "with rows outside")
+
+
+def test_attention_lengths_that_contradict_the_arrays(spd, h):
+    """query_start past the rows, decreasing, negative lengths: fewer tokens, never an access outside."""
+    w = World([(30, 4), (10, 6)], group=2, seed=9)
+    for starts, lens in (([0, 4, 100], [34, 16]), ([0, 8, 3], [34, 16]), ([-5, 4, 10], [34, 16]), ([0, 4, 10], [-3, 16])):
+        w.query_start, w.kv_lens = torch.tensor(starts, dtype=torch.int32), torch.tensor(lens, dtype=torch.int32)
+        out, lse = run_chunk(spd, h, w)
+        torch.cuda.synchronize()
+    w.query_start, w.kv_lens = torch.tensor([0, 4, 10], dtype=torch.int32), torch.tensor([-3, 16], dtype=torch.int32)
+    assert_close(w, run_chunk(spd, h, w), w.attention(), "a negative length")
+
+
+@pytest.mark.parametrize("rows", [(1, 8), (70, 1), (300, 1)])
+def test_attention_of_large_logits(spd, h, rows):
+    """Logits of hundreds: the maximum is what keeps the weights in range, and it moves late."""
+    n, group = rows
+    w = World([(400, n)], group=group, kv_heads=1, seed=12)
+    for number, j in ((int(w.table[0, j]), j) for j in range(pages_of(400 + n, 16))):
+        w.k[number] = (w.k[number].float() * (0.2 + 0.25 * j)).to(w.k.dtype)
+    out, lse = (x.double().cpu() for x in run_chunk(spd, h, w))
+    want, want_lse, room = w.attention()
+    # logits reach ~100: 128 products of fp32 sums are off by up to 128 * 2^-24 * sum |q k| <= 128 * 2^-24 * 900
+    tol = 128 * 2.0 ** -24 * 900
+    assert float((lse - want_lse).abs().max()) <= tol
+    assert bool(((out - want).abs() <= (2.0 ** -8 + tol) * (room + want.abs()) + 1e-12).all())
+
+
+def test_attention_of_a_cache_past_32_bits(spd, h):
+    """Pages whose elements lie past 2^32, from a cache of 10 GB."""
+    page, heads, dim = 1024, 8, 128
+    pages = (1 << 32) // (page * heads * dim) + 40
+    w = World([(2100, 2), (50, 1)], page=page, kv_heads=heads, group=2, seed=3, spare=0, wide=0)
+    k, v = (torch.empty((pages, page, heads, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    where = pages - 1 - torch.arange(w.pages)
+    k[where.cuda()], v[where.cuda()] = w.k.cuda(), w.v.cuda()
+    cache = spd.PagedCache(k, v, bounds=True)
+    table = torch.where(w.table >= 0, pages - 1 - w.table, -1)
+    batch = spd.PagedBatch(w.query_start.cuda(), w.kv_lens.cuda(), table.cuda())
+    want = w.attention()
+    assert_close(w, h.paged_attention(cache, w.queries(), batch), want, "past 32 bits")
+    out, lse, selected = h.paged_sparse_attention(cache, w.queries(), batch, 8)
+    assert_close(w, (out, lse), want, "past 32 bits, all pages selected")
+    last = torch.tensor([int(table[0, 2]) * page + 55], device="cuda")
+    new = torch.randn((1, heads, dim), dtype=torch.bfloat16, device="cuda")
+    h.paged_append(cache, new, new, last)
+    assert torch.equal(k[int(table[0, 2]), 55], new[0])
+
+
+def test_attention_equal_calls_give_equal_bits(spd, h):
+    w = World([(1000, 1), (70, 100), (3, 1)], seed=2)
+    cache, batch, q = w.cache(spd), w.batch(spd), w.queries()
+    first = [x.clone() for x in h.paged_attention(cache, q, batch)]
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, h.paged_attention(cache, q, batch)))
+
+
+# ------------------------------------------------------------------------------------------------ selected pages
+
+def check_sparse(spd, h, w, n_select, what):
+    w.make_bounds()
+    out, lse, selected = h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), n_select)
+    want = w.selection(n_select)
+    assert torch.equal(selected.cpu(), want), what
+    assert_close(w, (out, lse), w.attention(selected=want), what)
+
+
+@pytest.mark.parametrize("group", [1, 4, 5, 16, 20])
+@pytest.mark.parametrize("n_select", [2, 7, 33, 64])
+def test_sparse(spd, h, group, n_select):
+    requests = [(0, 1), (2500, 1), (1000, 3), (16 * n_select - 1, 2), (0, 20), (0, 0), (700, 1)]
+    w = World(requests, group=group, kv_heads=2, seed=group + n_select, drift=0.7, fused=True)
+    print("sparse", group, n_select, flush=True)
+    check_sparse(spd, h, w, n_select, "sparse")
+
+
+@pytest.mark.parametrize("dtype,dim,layout,page", [("bf16", 64, "htd", 32), ("f16", 128, "thd", 64), ("f16", 64, "htd", 16),
+                                                   ("bf16", 128, "htd", 128)])
+def test_sparse_types_and_layouts(spd, h, dtype, dim, layout, page):
+    w = World([(40 * page + 3, 2), (9 * page, 33), (0, 2)], dtype=dtype, dim=dim, layout=layout, page=page, group=3, seed=page, drift=1.0)
+    print("sparse", dtype, dim, layout, page, flush=True)
+    check_sparse(spd, h, w, 6, "sparse")
+
+
+def test_sparse_equal_scores_go_to_the_lower_page(spd, h):
+    """Every page holds the same keys, or nothing but zeros."""
+    for value in (1.0, 0.0):
+        w = World([(900, 2), (500, 1)], group=2, seed=6)
+        w.k = torch.where(torch.isnan(w.k.float()), w.k, torch.full_like(w.k, value))
+        check_sparse(spd, h, w, 5, "equal scores")
+        got = h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 5)[2].cpu()
+        assert got[0, 0].tolist() == [0, 1, 2, 3, 900 // 16]
+
+
+def test_sparse_pages_that_are_not_there_and_queries_of_zero(spd, h):
+    w = World([(600, 2), (300, 3), (20, 30)], group=2, seed=7, drift=0.5)
+    w.table[0, 5:30], w.table[1, 2], w.table[1, 0] = -1, w.pages + 3, -1
+    w.q[1] = 0
+    w.kv_lens[2] = 12                                                       # 18 rows see nothing
+    check_sparse(spd, h, w, 6, "missing pages")
+
+
+def test_sparse_of_many_tokens_and_a_wide_table(spd, h):
+    """More pages than a workgroup has lanes, and a chunk of tokens."""
+    w = World([(9000, 5), (120, 200)], kv_heads=1, group=2, dim=64, seed=10, drift=0.7)
+    check_sparse(spd, h, w, 16, "many pages")
+
+
+# ------------------------------------------------------------------------------------------------ together
+
+def serve(spd, h, steps, seed, n_select=0):
+    """A few requests from nothing: a prompt each, then tokens one by one, through all four calls, tables and slots
+    from the GPU.  Returns the last step's (world, outputs)."""
+    rng = np.random.default_rng(seed)
+    g = torch.Generator().manual_seed(seed)
+    page, heads, group, dim, n = 16, 2, 3, 64, 3
+    k, v = (torch.full((64, page, heads, dim), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    cache = spd.PagedCache(k, v, bounds=True)
+    table = torch.full((n, 20), -1, dtype=torch.int32, device="cuda")
+    free = torch.from_numpy(rng.permutation(64).astype(np.int32)).cuda()
+    past, keys, values = [0] * n, [[] for _ in range(n)], [[] for _ in range(n)]
+    for new in steps:
+        t = sum(new)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        b = h.paged_plan(i32(past), i32(new), free, table, page, t)
+        qkv = torch.randn((t, heads * group + 2 * heads, dim), generator=g).to(torch.bfloat16)
+        dev = qkv.cuda()
+        kn, vn = dev[:, heads * group:heads * group + heads], dev[:, heads * group + heads:]
+        h.paged_append(cache, kn, vn, b.slots)
+        got = h.paged_sparse_attention(cache, dev[:, :heads * group], b, n_select) if n_select else h.paged_attention(cache, dev[:, :heads * group], b)
+        torch.cuda.synchronize()
+        assert b.counts.tolist()[0] == t and b.counts.tolist()[2] == 0
+        free = free[b.counts.tolist()[1]:]
+        w = World([(p, m) for p, m in zip(past, new)], dim=dim, page=page, kv_heads=heads, group=group)
+        w.table, w.pages, w.k, w.v = table.cpu(), 64, k.cpu(), v.cpu()
+        w.q = qkv[:, :heads * group]
+        at = 0
+        for r, m in enumerate(new):
+            keys[r] += list(qkv[at:at + m, heads * group:heads * group + heads])
+            values[r] += list(qkv[at:at + m, heads * group + heads:])
+            at, past[r] = at + m, past[r] + m
+            for p in range(past[r]):                    # what lies where the table says
+                assert torch.equal(w.k[int(w.table[r, p // page]), p % page], keys[r][p])
+                assert torch.equal(w.v[int(w.table[r, p // page]), p % page], values[r][p])
+        selected = None
+        if n_select:
+            w.codes, w.code_scale = cache.codes.cpu(), cache.code_scale.cpu()
+            selected = w.selection(n_select)
+            assert torch.equal(got[2].cpu(), selected)
+        assert_close(w, got[:2], w.attention(selected=selected), "step %s" % (new,))
+
+
+@pytest.mark.parametrize("n_select", [0, 3])
+def test_steps_of_a_program(spd, h, n_select):
+    serve(spd, h, [[40, 0, 17], [1, 33, 1], [1, 1, 1], [20, 1, 0], [1, 1, 16], [1, 1, 1]], 5, n_select)
+
+
+def test_calls_follow_the_handles_stream(spd):
+    """A handle on a stream of its own: inputs made there, results read there."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        mine = spd.Handle()
+        serve(spd, mine, [[30, 1, 2], [1, 1, 1]], 6, 3)
+        stream.synchronize()
+        mine.close()
+
+
+def test_a_captured_step_replays(spd):
+    """plan, append and both attentions in one graph, replayed with other lengths and tokens, eager work between."""
+    page, heads, group, dim, n = 16, 2, 4, 128, 4
+    rng = np.random.default_rng(1)
+    k, v = (torch.zeros((200, page, heads, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        h = spd.Handle()
+        cache = spd.PagedCache(k, v, bounds=True)
+        table = torch.full((n, 40), -1, dtype=torch.int32, device="cuda")
+        free = torch.arange(200, dtype=torch.int32, device="cuda")
+        past, new = (torch.zeros(n, dtype=torch.int32, device="cuda") for _ in range(2))
+        qkv = torch.zeros((64, heads * (group + 2), dim), dtype=torch.bfloat16, device="cuda")
+        q, kn, vn = qkv[:, :heads * group], qkv[:, heads * group:heads * (group + 1)], qkv[:, heads * (group + 1):]
+        new += 3
+        b = h.paged_plan(past, new, free, table, page, 64)
+        scratch = torch.empty(max(h.paged_workspace_bytes(cache, b, 64, heads * group, s) for s in (0, 4)) + 256, dtype=torch.uint8, device="cuda")
+        h.set_workspace(scratch[(-scratch.data_ptr()) % 256:])
+
+        def step():
+            h.paged_plan(past, new, free, table, page, 64, out=b)
+            h.paged_append(cache, kn, vn, b.slots)
+            return h.paged_attention(cache, q, b) + h.paged_sparse_attention(cache, q, b, 4)
+
+        step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            kept = step()
+        done = np.zeros(n, np.int64)
+        for m in ([16, 9, 1, 30], [1, 1, 1, 1], [20, 1, 0, 16], [1, 0, 33, 2]):
+            qkv.copy_(torch.from_numpy(rng.standard_normal(tuple(qkv.shape)).astype(np.float32)))
+            past.copy_(torch.from_numpy(done.astype(np.int32)))
+            new.copy_(torch.tensor(m, dtype=torch.int32))
+            free.copy_(torch.from_numpy(rng.permutation(200).astype(np.int32)))
+            used = torch.unique(table[table >= 0])
+            free.copy_(torch.cat((free[~torch.isin(free, used)], free[torch.isin(free, used)])))
+            graph.replay()
+            stream.synchronize()
+            got = [x.clone() for x in kept]
+            eager = step()
+            stream.synchronize()
+            t = sum(m)
+            assert all(torch.equal(x[:t], y[:t]) for x, y in zip(got, eager))
+            done += np.asarray(m)
+            w = World([(int(d) - x, x) for d, x in zip(done, m)], page=page, kv_heads=heads, group=group)
+            w.table, w.pages, w.k, w.v, w.q = table.cpu(), 200, k.cpu(), v.cpu(), q[:t].cpu()
+            assert_close(w, [x[:t] for x in got[:2]], w.attention(), "replay")
+        h.set_workspace(None)
+        h.close()
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+
+def test_refusals_of_the_binding(spd, h):
+    w = World([(20, 2)], dim=64)
+    w.make_bounds()
+    cache, batch, q = w.cache(spd), w.batch(spd), w.queries()
+    bad = [lambda: spd.PagedCache(cache.k.float(), cache.v.float()), lambda: spd.PagedCache(cache.k, cache.v[:, :8]),
+           lambda: spd.PagedCache(cache.k, cache.v, cache.bounds), lambda: spd.PagedCache(cache.k.cpu(), cache.v.cpu()),
+           lambda: spd.PagedBatch(batch.query_start, batch.query_start, batch.block_table),
+           lambda: spd.PagedBatch(batch.query_start.long(), batch.kv_lens, batch.block_table),
+           lambda: h.paged_attention(cache, q.half(), batch), lambda: h.paged_attention(cache, q[:, :, :32], batch),
+           lambda: h.paged_attention(cache, q, batch, out=q[:1]), lambda: h.paged_attention(cache, q, batch, lse=q),
+           lambda: h.paged_append(cache, q[:, :2], q[:, :2], torch.zeros(2, dtype=torch.int32, device="cuda")),
+           lambda: h.paged_append(cache, q[:, :3], q[:, :3], torch.zeros(2, dtype=torch.int64, device="cuda"))]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail("not refused: %d" % i)
+
+
+def test_refusals_of_the_library(spd, h):
+    def refused(status, f):
+        with pytest.raises(spd.SpdError) as e:
+            f()
+        assert e.value.status_name == status and str(e.value), (status, e.value)
+
+    w = World([(20, 2)], dim=64, group=2)
+    w.make_bounds()
+    cache, batch, q = w.cache(spd), w.batch(spd), w.queries()
+    plain = spd.PagedCache(cache.k, cache.v)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    refused("SPD_ERR_DIM_MISMATCH", lambda: h.paged_attention(cache, q[:, :3], batch))                    # 3 heads on 2
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_attention(cache, q, batch, scale=scale))
+    for k in (0, 1, 65):
+        refused("SPD_ERR_BAD_K", lambda: h.paged_sparse_attention(cache, q, batch, k))
+    refused("SPD_ERR_NULL", lambda: h.paged_sparse_attention(plain, q, batch, 4))                         # no bounds
+    odd = torch.zeros((4, 24, 2, 64), dtype=torch.bfloat16, device="cuda")
+    refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_attention(spd.PagedCache(odd, odd), q, batch))          # pages of 24
+    narrow = torch.zeros((4, 16, 2, 96), dtype=torch.bfloat16, device="cuda")
+    refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_attention(spd.PagedCache(narrow, narrow), torch.zeros((2, 4, 96), dtype=torch.bfloat16, device="cuda"), batch))
+    skew = torch.zeros((4, 16, 2, 68), dtype=torch.bfloat16, device="cuda")[..., :64]
+    refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_attention(spd.PagedCache(skew, skew), q, batch))        # strides of 68
+    shifted = torch.zeros((2, 4, 72), dtype=torch.bfloat16, device="cuda")[..., 4:68]
+    refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_attention(cache, shifted, batch))                       # 8-byte aligned
+    for page in (0, 8, 48, 2048):
+        refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_plan(i32([1]), i32([1]), i32([1]), i32([[0]]), page, 1))
+    many = torch.zeros(16385, dtype=torch.int32, device="cuda")
+    refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_plan(many, many, i32([1]), many[:, None], 16, 1))
+    refused("SPD_ERR_DIM_MISMATCH", lambda: h.paged_plan(i32([1, 1]), i32([1, 1]), i32([1]), i32([[0, 1]]).expand(2, 2), 16, 1))
+    # too little scratch: refused before anything is enqueued, and the handle goes on
+    if (need := h.paged_workspace_bytes(cache, batch, 2, 4, 4)) > 256:
+        h.set_workspace(torch.empty(256, dtype=torch.uint8, device="cuda"))
+        refused("SPD_ERR_WORKSPACE", lambda: h.paged_sparse_attention(cache, q, batch, 4))
+        h.set_workspace(None)
+    assert need > 0
+    assert_close(w, h.paged_attention(cache, q, batch), w.attention(), "after the refusals")
+
+
+def test_nothing_to_do(spd, h):
+    w = World([(20, 2)], dim=64)
+    w.make_bounds()
+    cache, batch, q = w.cache(spd), w.batch(spd), w.queries()
+    out, lse = h.paged_attention(cache, q[:0], batch)
+    assert out.shape == (0, 8, 64) and lse.shape == (0, 8)
+    none = spd.PagedBatch(torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"),
+                          torch.zeros((0, 3), dtype=torch.int32, device="cuda"))
+    h.paged_attention(cache, q, none)
+    h.paged_sparse_attention(cache, q, none, 4)
+
+
+def test_profile_names_the_launches(spd):
+    w = World([(100, 2)], dim=64)
+    w.make_bounds()
+    h = spd.Handle()
+    h.set_option("profile", 1)
+    h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 4)
+    assert [r["name"] for r in h.profile_read()] == ["paged_select", "paged_attention"]
+    h.close()
