@@ -1,74 +1,823 @@
 // Attention of a chunk of new tokens over a paged cache, over all of its pages or over selected ones.
+#include <algorithm>
+
 #include "spd_paged_device.h"
 
 namespace spd {
 
 namespace {
 
-// A wavefront has one query row: two places (D = 128) or one of it to a lane, key after key, with the running maximum and sum of the
-// softmax.
-template <spd_dtype T, int D, bool SELECTED>
-__global__ void __launch_bounds__(256) spd_paged_attention_kernel(const PagedAttention a) {
-    using H = half_t<T>;
-    constexpr int E = D / 64;
-    const int lane = (int)threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
-    const int t = (int)(row / a.q.heads), h = (int)(row % a.q.heads), kvh = h / a.q.group;
-    if (t >= a.req.n_tokens) return;
-    const int r = paged_request_of(a.req, t);
-    if (r < 0) return;
-    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, r);
-    const int position = rq.kv - rq.count + (t - rq.first);
-    const int32_t *const table = a.req.block_table + (int64_t)r * a.req.table_stride;
-    float q[E], acc[E], top = -__builtin_inff(), sum = 0.0f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.0f;          // a row's maximum is moved (and its sums rescaled) once it grew by more than this: weights up to 2^8
+
+// ---- what there is to do -----------------------------------------------------------------------
+// The rows of a request and key head (tokens x query heads of it) are cut into tiles, a tile's keys into units; a tile and a key
+// head are a segment.  The segments' units in a row, key head by key head, are dealt to the workers in equal shares, whatever the
+// requests' lengths: a worker goes through whole segments and at most two parts of one, whose sums it leaves in scratch, where
+// another kernel joins them.
+
+struct Tile { int32_t request, row0, units, pad; };
+struct Schedule {
+    int64_t *first;                     // [tiles + 1]: units of the tiles before
+    Tile *tiles;
+    int64_t *request_tiles, *request_units;     // [requests]
+    int32_t *n_tiles;
+    int64_t most_tiles;                 // room; requests that overlap (which they may not) could have more
+    float *sums;                        // [2 * workers][rows of a tile * head_dim] of parts
+    float2 *stats;                      // [2 * workers][rows of a tile, as lanes have them]: maximum, sum
+};
+
+__device__ __forceinline__ int tile_units(const PagedRequest &rq, int group, int rows, int keys, int tile) {
+    const int last = min((tile + 1) * rows, rq.count * group) - 1, see = rq.kv - rq.count + last / group + 1;
+    return max(1, (see + keys - 1) / keys);             // (rows that see nothing are written too)
+}
+
+constexpr int kScheduleThreads = 1024;
+
+// One workgroup: a wavefront to a request counts its tiles and units, a scan over the requests, and the tiles are written.
+__global__ void __launch_bounds__(kScheduleThreads) spd_paged_schedule_kernel(const PagedRequests req, const int shift, const int group,
+                                                                               const int rows, const int keys, const Schedule s) {
+    __shared__ int64_t s_wave[kScheduleThreads / 64][2];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, n = req.n_requests;
+    for (int r = wave; r < n; r += kScheduleThreads / 64) {
+        const PagedRequest rq = paged_request(req, shift, r);
+        const int tiles = (rq.count * group + rows - 1) / rows;
+        int64_t units = 0;
+        for (int i = lane; i < tiles; i += 64) units += tile_units(rq, group, rows, keys, i);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        q[e] = (float)((const H *)a.q.ptr)[t * a.q.token_stride + h * a.q.head_stride + lane * E + e] * a.q.scale;
-        acc[e] = 0.0f;
+        for (int d = 32; d >= 1; d >>= 1) units += __shfl_xor(units, d);
+        if (lane == 0) { s.request_tiles[r] = tiles; s.request_units[r] = units; }
     }
-    const int pages = SELECTED ? a.n_select : (position >> a.cache.page_shift) + 1;
-    for (int i = 0; i < pages; ++i) {
-        const int col = SELECTED ? a.selected[((int64_t)t * a.cache.kv_heads + kvh) * a.n_select + i] : i;
-        if (col < 0) break;
-        const int32_t number = table[col];
-        if (number < 0 || number >= a.cache.n_pages) continue;
-        const int first = col << a.cache.page_shift, many = min(1 << a.cache.page_shift, position + 1 - first);
-        const int64_t at = number * a.cache.page_stride + kvh * a.cache.head_stride + lane * E;
-        for (int j = 0; j < many; ++j) {
-            const H *const k = (const H *)a.cache.k + at + j * a.cache.token_stride, *const v = (const H *)a.cache.v + at + j * a.cache.token_stride;
-            float x = 0.0f;
+    __threadfence_block();
+    __syncthreads();
+    int64_t tiles = 0, units = 0;
+    for (int base = 0; base < n; base += kScheduleThreads) {
+        const int r = base + tid;
+        const int64_t a = r < n ? s.request_tiles[r] : 0, b = r < n ? s.request_units[r] : 0;
+        int64_t ia = a, ib = b;
 #pragma unroll
-            for (int e = 0; e < E; ++e) x += q[e] * (float)k[e];
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t ua = __shfl_up(ia, d), ub = __shfl_up(ib, d);
+            if (lane >= d) { ia += ua; ib += ub; }
+        }
+        if (lane == 63) { s_wave[wave][0] = ia; s_wave[wave][1] = ib; }
+        __syncthreads();
+        int64_t ta = 0, tb = 0;
 #pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d);
-            const float now = fmaxf(top, x), old = exp2f(top - now), p = exp2f(x - now);
-            top = now;
-            sum = sum * old + p;
+        for (int w = 0; w < kScheduleThreads / 64; ++w) {
+            if (w < wave) { ia += s_wave[w][0]; ib += s_wave[w][1]; }
+            ta += s_wave[w][0]; tb += s_wave[w][1];
+        }
+        if (r < n) { s.request_tiles[r] = tiles + ia - a; s.request_units[r] = units + ib - b; }
+        tiles += ta; units += tb;
+        __syncthreads();
+    }
+    if (tid == 0) {
+        s.n_tiles[0] = (int32_t)min(tiles, s.most_tiles);
+        if (tiles <= s.most_tiles) s.first[tiles] = units;
+    }
+    __threadfence_block();
+    __syncthreads();
+    for (int r = wave; r < n; r += kScheduleThreads / 64) {
+        const PagedRequest rq = paged_request(req, shift, r);
+        const int many = (rq.count * group + rows - 1) / rows;
+        int64_t before = s.request_units[r];
+        const int64_t at = s.request_tiles[r];
+        for (int i0 = 0; i0 < many; i0 += 64) {
+            const int i = i0 + lane, u = i < many ? tile_units(rq, group, rows, keys, i) : 0;
+            int sum = u;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = acc[e] * old + p * (float)v[e];
+            for (int d = 1; d < 64; d <<= 1) { const int up = __shfl_up(sum, d); if (lane >= d) sum += up; }
+            if (i < many && at + i <= s.most_tiles) s.first[at + i] = before + sum - u;
+            if (i < many && at + i < s.most_tiles) s.tiles[at + i] = Tile{r, i * rows, u, 0};
+            before += __shfl(sum, 63);
         }
     }
+}
+
+// The share of worker `w` of `workers` in `all` units.
+__device__ __forceinline__ int64_t share_begin(int64_t all, int64_t workers, int64_t w) {
+    return all / workers * w + min(w, all % workers);
+}
+
+// As many workers as there are, but no fewer than `least` units to one.
+__device__ __forceinline__ int64_t workers_for(int64_t all, int64_t workers, int64_t least) { return max((int64_t)1, min(workers, all / least)); }
+
+struct Place { int64_t segment_begin; int tile, head; };        // segment_begin: its first unit's number
+
+// The segment that unit `at` is in: 64 lanes narrow the tiles down together.
+__device__ __forceinline__ Place find_place(const Schedule &s, int n_tiles, int64_t per_head, int64_t at) {
+    const int lane = (int)threadIdx.x & 63;
+    Place p;
+    p.head = (int)(at / per_head);
+    const int64_t x = at - p.head * per_head;
+    int lo = 0, hi = n_tiles;                                   // first[lo] <= x < first[hi]
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const uint64_t under = __ballot(i < hi && s.first[i] <= x);
+        lo += (63 - __builtin_clzll(under)) * step;
+        hi = min(hi, lo + step);
+    }
+    p.tile = uniform(lo);
+    p.segment_begin = p.head * per_head + s.first[p.tile];
+    return p;
+}
+
+// The pages of a request (or those selected), 64 at a time, a page's number to a lane.
+struct Pages {
+    const int32_t *list;                // numbers in the order of the walk
+    int n, now, after, block;           // block: which 64 of them `now` holds
+    __device__ __forceinline__ int load(int b) const {
+        const int i = b * 64 + ((int)threadIdx.x & 63);
+        return i < n ? list[i] : -1;
+    }
+    __device__ __forceinline__ void begin(const int32_t *l, int many, int at) {
+        list = l; n = many; block = at >> 6;
+        now = load(block);
+        after = load(block + 1);
+    }
+    __device__ __forceinline__ int number(int i) {              // i: uniform, not descending
+        if ((i >> 6) != block) { block = i >> 6; now = after; after = load(block + 1); }
+        return __builtin_amdgcn_readlane(now, i & 63);
+    }
+};
+
+// ---- few rows: a wavefront to 16 of them --------------------------------------------------------
+// Decoding, and selected pages: one to 16 rows, and every key is read once.  A wavefront is a worker of its own, and no barrier is in its
+// loop: 32 keys a unit, K straight from memory into the first product's operand, V through 8 KB of LDS from where it is
+// read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
+// lanes and order in which the second takes them, and a row is a lane's, its statistics too.
+
+constexpr int kNarrowRows = 16, kNarrowKeys = 32, kNarrowWaves = 4;
+
+struct NarrowPart {                     // of a segment
+    int request, first_token, count, position0;         // position0: where the request's first new token stands
+    int row0, rows;                     // of the tile in the request: its first, and how many are real
+    int head;
+    int subs;                           // 16-key steps that a row can see
+    int unit0, unit1;
+};
+
+template <spd_dtype T, int D, bool SELECTED>
+struct Narrow {
+    using H = half_t<T>;
+    using H8 = half8_t<T>;
+    static constexpr int kChunks = D / 8;               // 16 bytes each, of a row
+    static constexpr int kSteps = D / 32, kDims = D / 16, kVLoads = kNarrowKeys * kChunks / 64;
+    static constexpr int kRowsOfLoad = 64 / kChunks;    // rows of V in one load of the wavefront
+
+    H8 q[kSteps];
+    f32x4 o[kDims];
+    float top, sum;
+
+    // where V's chunk c of key row r lies in LDS: rows that are read together in different banks
+    static __device__ __forceinline__ int v_at(int r, int c) {
+        return r * D + (D == 128 ? (c ^ ((r & 3) << 2)) : (c ^ (((r >> 1) & 1) << 2))) * 8;
+    }
+
+    __device__ __forceinline__ void walk(const PagedAttention &a, const NarrowPart &p, H *lds) {
+        const int lane = (int)threadIdx.x & 63, row = lane & 15, quad = lane >> 4;
+        const int f = p.row0 + min(row, p.rows - 1), token = SELECTED ? 0 : f / a.q.group, g = SELECTED ? f : f - token * a.q.group;
+        const int position = p.position0 + token;
+        {
+            const H *const from = (const H *)a.q.ptr + (int64_t)(p.first_token + token) * a.q.token_stride +
+                                  ((int64_t)p.head * a.q.group + g) * a.q.head_stride + quad * 8;
 #pragma unroll
-    for (int e = 0; e < E; ++e) ((H *)a.out.out)[((int64_t)t * a.q.heads + h) * D + lane * E + e] = (H)(sum > 0.0f ? acc[e] / sum : 0.0f);
-    if (lane == 0 && a.out.lse) a.out.lse[(int64_t)t * a.q.heads + h] = sum > 0.0f ? (top + log2f(sum)) * 0.6931471805599453f : -__builtin_inff();
+            for (int s = 0; s < kSteps; ++s) q[s] = *(const H8 *)(from + s * 32);
+        }
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
+        top = -__builtin_inff(); sum = 0.0f;
+        const int shift = a.cache.page_shift, per_page = shift - 4;
+        // the places of the first row (the least) and of the last
+        const int least = p.position0 + (SELECTED ? 0 : p.row0 / a.q.group), most = p.position0 + (SELECTED ? 0 : (p.row0 + p.rows - 1) / a.q.group);
+        const int32_t *const table = a.req.block_table + (int64_t)p.request * a.req.table_stride;
+        Pages pages;
+        int chosen = -1, chosen_number = -1;            // SELECTED: the list, a page to a lane
+        if (SELECTED) {
+            const int32_t *const list = a.selected + ((int64_t)p.first_token * a.cache.kv_heads + p.head) * a.n_select;
+            if (lane < a.n_select) chosen = list[lane];
+            if (chosen >= 0) chosen_number = table[chosen];
+        } else {
+            pages.begin(table, a.req.max_pages, (p.unit0 * 2) >> per_page);
+        }
+        H8 kr[2][kSteps], vr[kVLoads];
+        int pos0[2], here[2];                           // of the two 16-key steps: the first key's position, and whether the page is there
+        int64_t base[2];
+        auto locate = [&](int u, int *pos, int *ok, int64_t *at) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int s = 2 * u + j, i = s >> per_page, in = (s & ((1 << per_page) - 1)) << 4;
+                int number, col;
+                if (SELECTED) { col = __builtin_amdgcn_readlane(chosen, i & 63); number = __builtin_amdgcn_readlane(chosen_number, i & 63); }
+                else { col = i; number = pages.number(i); }
+                ok[j] = s < p.subs && number >= 0 && number < a.cache.n_pages;
+                pos[j] = (col << shift) + in;
+                at[j] = (int64_t)number * a.cache.page_stride + (int64_t)in * a.cache.token_stride + (int64_t)p.head * a.cache.head_stride;
+            }
+        };
+        const int64_t k_lane = (int64_t)row * a.cache.token_stride + quad * 8;
+        const int v_row = lane / kChunks, v_chunk = lane % kChunks;
+        auto fetch = [&](const int *ok, const int64_t *at) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (!ok[j]) continue;
+                const H *const k = (const H *)a.cache.k + at[j] + k_lane;
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) kr[j][s] = *(const H8 *)(k + s * 32);
+                const H *const v = (const H *)a.cache.v + at[j] + (int64_t)v_row * a.cache.token_stride + v_chunk * 8;
+#pragma unroll
+                for (int i = 0; i < kVLoads / 2; ++i) vr[j * (kVLoads / 2) + i] = *(const H8 *)(v + (int64_t)(i * kRowsOfLoad) * a.cache.token_stride);
+            }
+        };
+        H8 zero;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) zero[i] = (H)0.0f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) kr[j][s] = zero;
+#pragma unroll
+        for (int i = 0; i < kVLoads; ++i) vr[i] = zero;
+        locate(p.unit0, pos0, here, base);
+        fetch(here, base);
+        for (int u = p.unit0; u < p.unit1; ++u) {
+            int pos_next[2] = {0, 0}, here_next[2] = {0, 0};
+            int64_t base_next[2] = {0, 0};
+            if (u + 1 < p.unit1) locate(u + 1, pos_next, here_next, base_next);
+            // V into LDS; what no row of the tile sees becomes 0, since 0 times what lies there need not be
+#pragma unroll
+            for (int i = 0; i < kVLoads; ++i) {
+                const int j = i / (kVLoads / 2), r = (i % (kVLoads / 2)) * kRowsOfLoad + v_row;
+                if (!here[j] || pos0[j] + 15 > most) { if (!here[j] || pos0[j] + r > most) vr[i] = zero; }
+                *(H8 *)(lds + v_at(j * 16 + r, v_chunk)) = vr[i];
+            }
+            f32x4 x[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                x[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) x[j] = mfma16(kr[j][s], q[s], x[j]);
+            }
+            const int now_pos[2] = {pos0[0], pos0[1]}, now_here[2] = {here[0], here[1]};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) { pos0[j] = pos_next[j]; here[j] = here_next[j]; base[j] = base_next[j]; }
+            fetch(here, base);
+            // weights, a row's keys 4 quad + i of either step
+            float w[8];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[j * 4 + i] = x[j][i] * a.q.scale;
+                if (!now_here[j] || now_pos[j] + 15 > least)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (!now_here[j] || now_pos[j] + quad * 4 + i > position) w[j * 4 + i] = -__builtin_inff();
+            }
+            float big = w[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
+            big = fmaxf(big, __shfl_xor(big, 16));
+            big = fmaxf(big, __shfl_xor(big, 32));
+            if (__any(big > top + kSlack)) {
+                const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+                top = to;
+                sum *= old;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[d] *= old;
+            }
+            const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(w[i] - from); sum += w[i]; }
+            const H8 pw = rounded<T>(w);
+            const int s = lane & 15;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) {
+                half4_t<T> part[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int r = j * 16 + quad * 4 + (s >> 2);
+                    part[j] = read_transposed<T>(lds + v_at(r, d * 2 + ((s & 3) >> 1)) + (s & 1) * 4);
+                }
+                const H8 v = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                o[d] = mfma16(v, pw, o[d]);
+            }
+        }
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+    }
+
+    __device__ __forceinline__ void write(const PagedAttention &a, const NarrowPart &p) const {
+        const int lane = (int)threadIdx.x & 63, row = lane & 15, quad = lane >> 4;
+        if (row >= p.rows) return;
+        const int f = p.row0 + row, token = SELECTED ? 0 : f / a.q.group, g = SELECTED ? f : f - token * a.q.group;
+        const int64_t at = (int64_t)(p.first_token + token) * a.q.heads + (int64_t)p.head * a.q.group + g;
+        const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            half4_t<T> r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = (H)(o[d][i] * by);
+            *(half4_t<T> *)((H *)a.out.out + at * D + d * 16 + quad * 4) = r;
+        }
+        if (quad == 0 && a.out.lse) a.out.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+    }
+
+    __device__ __forceinline__ void leave(const Schedule &s, int64_t slot) const {
+        const int lane = (int)threadIdx.x & 63;
+        f32x4 *const to = (f32x4 *)(s.sums + slot * (kNarrowRows * D));
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) to[d * 64 + lane] = o[d];
+        s.stats[slot * 64 + lane] = make_float2(top, sum);
+    }
+
+    // Takes in the part in `slot`.
+    __device__ __forceinline__ void join(const Schedule &s, int64_t slot) {
+        const int lane = (int)threadIdx.x & 63;
+        const float2 st = s.stats[slot * 64 + lane];
+        const f32x4 *const from = (const f32x4 *)(s.sums + slot * (kNarrowRows * D));
+        const float to = fmaxf(top, st.x), mine = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - to),
+                    theirs = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.x - to);
+        top = to;
+        sum = sum * mine + st.y * theirs;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[d] = o[d] * mine + from[d * 64 + lane] * theirs;
+    }
+
+    __device__ __forceinline__ void clear() {
+        top = -__builtin_inff(); sum = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
+    }
+};
+
+__device__ __forceinline__ NarrowPart narrow_part(const PagedAttention &a, const Tile &t, int head) {
+    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, t.request);
+    NarrowPart p;
+    p.request = t.request;
+    p.first_token = rq.first; p.count = rq.count; p.position0 = rq.kv - rq.count;
+    p.row0 = t.row0;
+    p.rows = min(kNarrowRows, rq.count * a.q.group - t.row0);
+    p.head = head;
+    const int see = p.position0 + (t.row0 + p.rows - 1) / a.q.group + 1;
+    p.subs = max(0, (see + 15) / 16);
+    return p;
 }
 
 template <spd_dtype T, int D>
-void start(hipStream_t st, const PagedAttention &a) {
-    const dim3 grid((unsigned)(((int64_t)a.req.n_tokens * a.q.heads + 3) / 4));
-    if (a.selected) hipLaunchKernelGGL((spd_paged_attention_kernel<T, D, true>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((spd_paged_attention_kernel<T, D, false>), grid, dim3(256), 0, st, a);
+__global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(const PagedAttention a, const Schedule s) {
+    __shared__ __align__(16) half_t<T> s_v[kNarrowWaves][kNarrowKeys * D];
+    const int wave = uniform((int)threadIdx.x >> 6), n_tiles = s.n_tiles[0];
+    if (n_tiles == 0) return;
+    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads;
+    const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves, 1);
+    // neighbours in the units' order share an XCD and its L2 (workgroups go to the XCDs in turn)
+    const int64_t group = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = group * kNarrowWaves + wave;
+    if (w >= workers) return;
+    int64_t at = share_begin(all, workers, w);
+    const int64_t end = share_begin(all, workers, w + 1);
+    Place place = find_place(s, n_tiles, per_head, at);
+    while (at < end) {
+        const Tile t = s.tiles[place.tile];
+        NarrowPart p = narrow_part(a, Tile{uniform(t.request), uniform(t.row0), uniform(t.units), 0}, place.head);
+        p.unit0 = (int)(at - place.segment_begin);
+        p.unit1 = (int)min((int64_t)t.units, end - place.segment_begin);
+        p.unit0 = uniform(p.unit0); p.unit1 = uniform(p.unit1);
+        Narrow<T, D, false> n;
+        n.walk(a, p, s_v[wave]);
+        if (p.unit0 == 0 && p.unit1 == t.units) n.write(a, p);
+        else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
+        at = place.segment_begin + p.unit1;
+        if (p.unit1 == t.units) {
+            place.segment_begin = at;
+            if (++place.tile == n_tiles) { place.tile = 0; ++place.head; }
+        }
+    }
+}
+
+// The first worker that begins inside a segment joins the segment's parts.
+template <spd_dtype T, int D>
+__global__ void __launch_bounds__(64) spd_paged_narrow_join_kernel(const PagedAttention a, const Schedule s, const int most_workers) {
+    const int n_tiles = s.n_tiles[0];
+    if (n_tiles == 0) return;
+    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads, workers = workers_for(all, most_workers, 1);
+    const int64_t w = (int64_t)blockIdx.x + 1;
+    if (w >= workers) return;
+    const int64_t at = share_begin(all, workers, w);
+    const Place place = find_place(s, n_tiles, per_head, at);
+    if (at == place.segment_begin || share_begin(all, workers, w - 1) > place.segment_begin) return;
+    const Tile t = s.tiles[place.tile];
+    const int64_t end = place.segment_begin + t.units;
+    Narrow<T, D, false> n;
+    n.clear();
+    n.join(s, 2 * (w - 1) + 1);
+    for (int64_t other = w; other < workers && share_begin(all, workers, other) < end; ++other) n.join(s, 2 * other);
+    n.write(a, narrow_part(a, t, place.head));
+}
+
+// Selected pages: a segment is a token, a key head and 16 of its query heads, cut into `splits` equal parts.
+template <spd_dtype T, int D, bool JOIN>
+__global__ void __launch_bounds__(JOIN ? 64 : kNarrowWaves * 64, JOIN ? 1 : 2)
+    spd_paged_selected_kernel(const PagedAttention a, const Schedule s, const int splits, const int head_tiles) {
+    __shared__ __align__(16) half_t<T> s_v[JOIN ? 1 : kNarrowWaves][JOIN ? 8 : kNarrowKeys * D];
+    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    // (a token's and its neighbours' segments share pages: neighbours share an XCD)
+    const int64_t blocks = (int64_t)gridDim.x, per = blocks / 8, rest = blocks % 8, xcd = blockIdx.x % 8;
+    const int64_t block = JOIN ? (int64_t)blockIdx.x : xcd * per + min(xcd, rest) + blockIdx.x / 8;
+    const int64_t w = JOIN ? block : block * kNarrowWaves + wave;
+    const int64_t segment = JOIN ? w : w / splits;
+    const int split = JOIN ? 0 : (int)(w % splits);
+    const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * head_tiles;
+    if (segment >= segments) return;
+    const int tile = (int)(segment % head_tiles);
+    const int64_t rest_of = segment / head_tiles;
+    const int token = (int)(rest_of % a.req.n_tokens), head = (int)(rest_of / a.req.n_tokens);
+    const int r = paged_request_of(a.req, token);
+    if (r < 0) return;
+    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, r);
+    NarrowPart p;
+    p.request = uniform(r);
+    p.first_token = uniform(token); p.count = 1;
+    p.position0 = uniform(rq.kv - rq.count + token - rq.first);
+    p.row0 = tile * kNarrowRows;
+    p.rows = min(kNarrowRows, a.q.group - p.row0);
+    p.head = uniform(head);
+    // pages in the list, the last of which is the token's own
+    const int32_t *const list = a.selected + ((int64_t)token * a.cache.kv_heads + head) * a.n_select;
+    const int many = __popcll(__ballot(lane < a.n_select && list[lane] >= 0));
+    const int shift = a.cache.page_shift;
+    p.subs = many == 0 ? 0 : uniform(((many - 1) << (shift - 4)) + ((p.position0 & ((1 << shift) - 1)) >> 4) + 1);
+    const int units = max(1, (p.subs + 1) / 2);
+    Narrow<T, D, true> n;
+    if (JOIN) {
+        n.clear();
+        for (int i = 0; i < splits; ++i) if (share_begin(units, splits, i + 1) > share_begin(units, splits, i)) n.join(s, segment * splits + i);
+        n.write(a, p);
+        return;
+    }
+    p.unit0 = uniform((int)share_begin(units, splits, split));
+    p.unit1 = uniform((int)share_begin(units, splits, split + 1));
+    if (p.unit0 == p.unit1) return;
+    n.walk(a, p, s_v[JOIN ? 0 : wave]);
+    if (splits == 1) n.write(a, p); else n.leave(s, w);
+}
+
+// ---- many rows: a workgroup to 128 of them -------------------------------------------------------
+
+constexpr int kWideRows = 128, kWideKeys = 64, kWideWaves = 4;
+
+struct WidePart {
+    int request, first_token, position0, row0, rows, head;
+    int see;                            // keys that the tile's last row sees
+    int unit0, unit1;
+};
+
+template <spd_dtype T, int D>
+struct Wide {
+    using H = half_t<T>;
+    using H8 = half8_t<T>;
+    static constexpr int kChunks = D / 8, kSteps = D / 16, kDims = D / 32;
+    static constexpr int kRowsOfLoad = kWideWaves * 64 / kChunks, kLoads = kWideKeys / kRowsOfLoad;
+    static constexpr int kTile = kWideKeys * D;         // values of K or V in LDS
+
+    H8 q[kSteps];
+    f32x16 o[kDims];
+    float top, sum;
+
+    static __device__ __forceinline__ int k_at(int r, int c) { return r * D + (D == 128 ? (c ^ (r & 15)) : (c ^ ((r >> 1) & 7))) * 8; }
+    static __device__ __forceinline__ int v_at(int r, int c) {
+        return r * D + (D == 128 ? (c ^ ((r & 3) << 2)) : (c ^ (((r >> 1) & 1) << 2))) * 8;
+    }
+
+    __device__ __forceinline__ void clear() {
+        top = -__builtin_inff(); sum = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    }
+
+    // lds: two buffers of K and V
+    __device__ __forceinline__ void walk(const PagedAttention &a, const WidePart &p, H *lds) {
+        const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
+        const int mine = wave * 32 + (lane & 31), f = p.row0 + min(mine, p.rows - 1), token = f / a.q.group, g = f - token * a.q.group;
+        const int position = p.position0 + token;
+        {
+            const H *const from = (const H *)a.q.ptr + (int64_t)(p.first_token + token) * a.q.token_stride +
+                                  ((int64_t)p.head * a.q.group + g) * a.q.head_stride + half * 8;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) q[s] = *(const H8 *)(from + s * 16);
+        }
+        clear();
+        const int shift = a.cache.page_shift;
+        const bool busy = wave * 32 < p.rows;           // this wavefront has rows
+        const int least = p.position0 + (p.row0 + min(wave * 32, p.rows - 1)) / a.q.group,
+                  most = p.position0 + (p.row0 + min(wave * 32 + 31, p.rows - 1)) / a.q.group;
+        Pages pages;
+        pages.begin(a.req.block_table + (int64_t)p.request * a.req.table_stride, a.req.max_pages, (p.unit0 * kWideKeys) >> shift);
+        const int l_row = tid / kChunks, l_chunk = tid % kChunks;
+        H8 kr[kLoads], vr[kLoads];
+        uint64_t there = 0, there_next;                 // keys of the unit whose page is there
+        H8 zero;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) zero[i] = (H)0.0f;
+        auto fetch = [&](int u) {
+            there_next = 0;
+            int number[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {               // 16 keys lie in one page
+                const int i = (u * kWideKeys + j * 16) >> shift;
+                number[j] = pages.number(i);
+                const bool ok = number[j] >= 0 && number[j] < a.cache.n_pages && u * kWideKeys + j * 16 < p.see;
+                there_next |= ok ? 0xffffull << (16 * j) : 0;
+            }
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                const int r = l * kRowsOfLoad + l_row, key = u * kWideKeys + r;
+                int j = 0, which = number[0];
+                if (D == 128) { j = l; which = number[l]; }
+                else { j = 2 * l + (wave >> 1); which = wave >> 1 ? number[2 * l + 1 < 4 ? 2 * l + 1 : 3] : number[2 * l < 4 ? 2 * l : 3]; }
+                const bool ok = (there_next >> (16 * j)) & 1;
+                kr[l] = zero; vr[l] = zero;
+                if (ok && key < p.see) {
+                    const int64_t at = (int64_t)which * a.cache.page_stride + (int64_t)(key & ((1 << shift) - 1)) * a.cache.token_stride +
+                                       (int64_t)p.head * a.cache.head_stride + l_chunk * 8;
+                    kr[l] = *(const H8 *)((const H *)a.cache.k + at);
+                    vr[l] = *(const H8 *)((const H *)a.cache.v + at);
+                }
+            }
+        };
+        auto store = [&](int buffer) {
+            H *const k = lds + buffer * 2 * kTile, *const v = k + kTile;
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                const int r = l * kRowsOfLoad + l_row;
+                *(H8 *)(k + k_at(r, l_chunk)) = kr[l];
+                *(H8 *)(v + v_at(r, l_chunk)) = vr[l];
+            }
+        };
+        fetch(p.unit0);
+        there = there_next;
+        store(0);
+        __syncthreads();
+        for (int u = p.unit0; u < p.unit1; ++u) {
+            const int buffer = (u - p.unit0) & 1;
+            const bool more = u + 1 < p.unit1;
+            if (more) fetch(u + 1);
+            const int key0 = u * kWideKeys;
+            if (busy && key0 <= most) {
+                const H *const k = lds + buffer * 2 * kTile, *const v = k + kTile;
+                f32x16 x[2];
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[t][i] = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) x[t] = mfma32(*(const H8 *)(k + k_at(t * 32 + (lane & 31), 2 * s + half)), q[s], x[t]);
+                }
+                float w[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) w[i] = x[i >> 4][i & 15] * a.q.scale;
+                if (key0 + kWideKeys - 1 > least || there != ~0ull) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int c = (i >> 4) * 32 + ((i & 15) >> 2) * 8 + half * 4 + (i & 3);
+                        if (key0 + c > position || !((there >> c) & 1)) w[i] = -__builtin_inff();
+                    }
+                }
+                float big = w[0];
+#pragma unroll
+                for (int i = 1; i < 32; ++i) big = fmaxf(big, w[i]);
+                big = fmaxf(big, __shfl_xor(big, 32));
+                if (__any(big > top + kSlack)) {
+                    const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+                    top = to;
+                    sum *= old;
+#pragma unroll
+                    for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[d][i] *= old;
+                }
+                const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) { w[i] = __builtin_amdgcn_exp2f(w[i] - from); sum += w[i]; }
+                const int s = lane & 15;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {           // 16 keys
+                    const H8 pw = rounded<T>(w + e * 8);
+#pragma unroll
+                    for (int d = 0; d < kDims; ++d) {
+                        half4_t<T> part[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int r = e * 16 + j * 8 + half * 4 + (s >> 2);
+                            part[j] = read_transposed<T>(v + v_at(r, d * 4 + ((lane >> 4) & 1) * 2 + ((s & 3) >> 1)) + (s & 1) * 4);
+                        }
+                        o[d] = mfma32(__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7), pw, o[d]);
+                    }
+                }
+            }
+            if (more) { store(buffer ^ 1); there = there_next; }
+            __syncthreads();
+        }
+        sum += __shfl_xor(sum, 32);
+    }
+
+    __device__ __forceinline__ void write(const PagedAttention &a, const WidePart &p) const {
+        const int lane = (int)threadIdx.x & 63, half = lane >> 5, mine = ((int)threadIdx.x >> 6) * 32 + (lane & 31);
+        if (mine >= p.rows) return;
+        const int f = p.row0 + mine, token = f / a.q.group, g = f - token * a.q.group;
+        const int64_t at = (int64_t)(p.first_token + token) * a.q.heads + (int64_t)p.head * a.q.group + g;
+        const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                half4_t<T> r;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = (H)(o[d][i * 4 + e] * by);
+                *(half4_t<T> *)((H *)a.out.out + at * D + d * 32 + i * 8 + half * 4) = r;
+            }
+        if (half == 0 && a.out.lse) a.out.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+    }
+
+    __device__ __forceinline__ void leave(const Schedule &s, int64_t slot) const {
+        const int tid = (int)threadIdx.x;
+        f32x4 *const to = (f32x4 *)(s.sums + slot * (kWideRows * D));
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[(d * 4 + i) * 256 + tid] = f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
+        s.stats[slot * 256 + tid] = make_float2(top, sum);
+    }
+
+    __device__ __forceinline__ void join(const Schedule &s, int64_t slot) {
+        const int tid = (int)threadIdx.x;
+        const float2 st = s.stats[slot * 256 + tid];
+        const f32x4 *const from = (const f32x4 *)(s.sums + slot * (kWideRows * D));
+        const float to = fmaxf(top, st.x), mine = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - to),
+                    theirs = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.x - to);
+        top = to;
+        sum = sum * mine + st.y * theirs;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 x = from[(d * 4 + i) * 256 + tid];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][i * 4 + e] = o[d][i * 4 + e] * mine + x[e] * theirs;
+            }
+    }
+};
+
+__device__ __forceinline__ WidePart wide_part(const PagedAttention &a, const Tile &t, int head) {
+    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, t.request);
+    WidePart p;
+    p.request = uniform(t.request);
+    p.first_token = uniform(rq.first); p.position0 = uniform(rq.kv - rq.count);
+    p.row0 = uniform(t.row0);
+    p.rows = uniform(min(kWideRows, rq.count * a.q.group - t.row0));
+    p.head = uniform(head);
+    p.see = max(0, p.position0 + (p.row0 + p.rows - 1) / a.q.group + 1);
+    return p;
+}
+
+template <spd_dtype T, int D>
+__global__ void __launch_bounds__(kWideWaves * 64, 2) spd_paged_wide_kernel(const PagedAttention a, const Schedule s) {
+    __shared__ __align__(16) half_t<T> s_kv[4 * kWideKeys * D];
+    const int n_tiles = s.n_tiles[0];
+    if (n_tiles == 0) return;
+    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads, workers = workers_for(all, gridDim.x, 1);
+    const int64_t w = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+    if (w >= workers) return;
+    int64_t at = share_begin(all, workers, w);
+    const int64_t end = share_begin(all, workers, w + 1);
+    Place place = find_place(s, n_tiles, per_head, at);
+    while (at < end) {
+        const Tile t = s.tiles[place.tile];
+        WidePart p = wide_part(a, t, place.head);
+        p.unit0 = uniform((int)(at - place.segment_begin));
+        p.unit1 = uniform((int)min((int64_t)t.units, end - place.segment_begin));
+        Wide<T, D> n;
+        n.walk(a, p, s_kv);
+        if (p.unit0 == 0 && p.unit1 == t.units) n.write(a, p);
+        else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
+        at = place.segment_begin + p.unit1;
+        if (p.unit1 == t.units) {
+            place.segment_begin = at;
+            if (++place.tile == n_tiles) { place.tile = 0; ++place.head; }
+        }
+    }
+}
+
+template <spd_dtype T, int D>
+__global__ void __launch_bounds__(kWideWaves * 64) spd_paged_wide_join_kernel(const PagedAttention a, const Schedule s, const int most_workers) {
+    const int n_tiles = s.n_tiles[0];
+    if (n_tiles == 0) return;
+    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads, workers = workers_for(all, most_workers, 1);
+    const int64_t w = (int64_t)blockIdx.x + 1;
+    if (w >= workers) return;
+    const int64_t at = share_begin(all, workers, w);
+    const Place place = find_place(s, n_tiles, per_head, at);
+    if (at == place.segment_begin || share_begin(all, workers, w - 1) > place.segment_begin) return;
+    const Tile t = s.tiles[place.tile];
+    const int64_t end = place.segment_begin + t.units;
+    Wide<T, D> n;
+    n.clear();
+    n.join(s, 2 * (w - 1) + 1);
+    for (int64_t other = w; other < workers && share_begin(all, workers, other) < end; ++other) n.join(s, 2 * other);
+    n.write(a, wide_part(a, t, place.head));
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+
+size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+struct Cut {
+    bool wide;
+    int rows, keys, workers, threads;   // threads: of a worker
+    int splits, head_tiles;             // of selected segments
+    int64_t tiles;                      // at most
+};
+
+Cut cut_of(const PagedAttention &a, int n_cus) {
+    Cut c{};
+    const int64_t rows = (int64_t)a.req.n_tokens * a.q.heads / a.cache.kv_heads;        // of one key head
+    if (a.selected) {
+        c.rows = kNarrowRows; c.keys = kNarrowKeys; c.threads = 64;
+        c.head_tiles = (a.q.group + kNarrowRows - 1) / kNarrowRows;
+        const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles;
+        const int64_t units = std::max<int64_t>(1, ((int64_t)a.n_select << a.cache.page_shift) / kNarrowKeys);
+        const int64_t want = (int64_t)n_cus * 8;
+        c.splits = (int)std::max<int64_t>(1, std::min(units, want / std::max<int64_t>(segments, 1)));
+        c.workers = 0;
+        return c;
+    }
+    c.wide = rows > 24 * (int64_t)a.req.n_requests;
+    c.rows = c.wide ? kWideRows : kNarrowRows;
+    c.keys = c.wide ? kWideKeys : kNarrowKeys;
+    c.threads = c.wide ? kWideWaves * 64 : 64;
+    const int groups = std::max(n_cus / 8, 1) * 8 * 2;      // two to a compute unit, as many to every XCD
+    c.workers = c.wide ? groups : groups * kNarrowWaves;
+    c.tiles = rows / c.rows + a.req.n_requests;
+    return c;
+}
+
+// The schedule's arrays in the scratch at `base` (which may be null), and the bytes they take.
+size_t lay_out(const PagedAttention &a, const Cut &c, unsigned char *base, Schedule *s) {
+    size_t at = 0;
+    auto take = [&](size_t bytes) { unsigned char *const p = base ? base + at : nullptr; at += align256(bytes); return p; };
+    size_t slots = 0;
+    if (a.selected) {
+        slots = c.splits > 1 ? (size_t)a.req.n_tokens * (size_t)a.cache.kv_heads * (size_t)c.head_tiles * (size_t)c.splits : 0;
+    } else {
+        s->n_tiles = (int32_t *)take(4);
+        s->first = (int64_t *)take((size_t)(c.tiles + 1) * 8);
+        s->most_tiles = c.tiles;
+        s->tiles = (Tile *)take((size_t)c.tiles * sizeof(Tile));
+        s->request_tiles = (int64_t *)take((size_t)a.req.n_requests * 8);
+        s->request_units = (int64_t *)take((size_t)a.req.n_requests * 8);
+        slots = 2 * (size_t)c.workers;
+    }
+    s->sums = (float *)take(slots * (size_t)c.rows * (size_t)a.head_dim * 4);
+    s->stats = (float2 *)take(slots * (size_t)c.threads * 8);
+    return at;
+}
+
+template <spd_dtype T, int D>
+hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Schedule &s) {
+    if (a.selected) {
+        const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles, waves = segments * c.splits;
+        hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, false>), dim3((unsigned)((waves + kNarrowWaves - 1) / kNarrowWaves)),
+                           dim3(kNarrowWaves * 64), 0, st, a, s, c.splits, c.head_tiles);
+        if (c.splits > 1)
+            hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, true>), dim3((unsigned)segments), dim3(64), 0, st, a, s, c.splits, c.head_tiles);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(spd_paged_schedule_kernel, dim3(1), dim3(kScheduleThreads), 0, st, a.req, a.cache.page_shift, a.q.group, c.rows, c.keys, s);
+    if (c.wide) {
+        hipLaunchKernelGGL((spd_paged_wide_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s);
+        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s, c.workers);
+    } else {
+        hipLaunchKernelGGL((spd_paged_narrow_kernel<T, D>), dim3((unsigned)(c.workers / kNarrowWaves)), dim3(kNarrowWaves * 64), 0, st, a, s);
+        hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(64), 0, st, a, s, c.workers);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t paged_attention_scratch(const PagedAttention &, int) { return 0; }
+size_t paged_attention_scratch(const PagedAttention &a, int n_cus) {
+    Schedule s{};
+    return lay_out(a, cut_of(a, n_cus), nullptr, &s);
+}
 
-hipError_t launch_paged_attention(hipStream_t st, const PagedAttention &a, void *, int) {
+hipError_t launch_paged_attention(hipStream_t st, const PagedAttention &a, void *scratch, int n_cus) {
     if (a.req.n_tokens == 0) return hipSuccess;
-    if (a.dtype == SPD_BF16) { if (a.head_dim == 64) start<SPD_BF16, 64>(st, a); else start<SPD_BF16, 128>(st, a); }
-    else { if (a.head_dim == 64) start<SPD_F16, 64>(st, a); else start<SPD_F16, 128>(st, a); }
-    return hipGetLastError();
+    const Cut c = cut_of(a, n_cus);
+    Schedule s{};
+    lay_out(a, c, static_cast<unsigned char *>(scratch), &s);
+    if (a.dtype == SPD_BF16) return a.head_dim == 64 ? start<SPD_BF16, 64>(st, a, c, s) : start<SPD_BF16, 128>(st, a, c, s);
+    return a.head_dim == 64 ? start<SPD_F16, 64>(st, a, c, s) : start<SPD_F16, 128>(st, a, c, s);
 }
 
 }  // namespace spd
