@@ -330,17 +330,37 @@ struct Narrow {
         s.stats[slot * 64 + lane] = make_float2(top, sum);
     }
 
-    // Takes in the part in `slot`.
-    __device__ __forceinline__ void join(const Schedule &s, int64_t slot) {
-        const int lane = (int)threadIdx.x & 63;
-        const float2 st = s.stats[slot * 64 + lane];
-        const f32x4 *const from = (const f32x4 *)(s.sums + slot * (kNarrowRows * D));
+    // Takes in another part's sums.
+    __device__ __forceinline__ void take(const float2 st, const f32x4 (*from)[64], int lane) {
         const float to = fmaxf(top, st.x), mine = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - to),
                     theirs = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.x - to);
         top = to;
         sum = sum * mine + st.y * theirs;
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) o[d] = o[d] * mine + from[d * 64 + lane] * theirs;
+        for (int d = 0; d < kDims; ++d) o[d] = o[d] * mine + from[d][lane] * theirs;
+    }
+
+    // Of `many` parts in slots slot(0), slot(1), ... those from `first` on, `step` apart; two are in flight.
+    template <typename Slot>
+    __device__ __forceinline__ void join_all(const Schedule &s, int many, int first, int step, Slot slot) {
+        const int lane = (int)threadIdx.x & 63;
+        auto sums = [&](int64_t at) { return (const f32x4 (*)[64])(s.sums + at * (kNarrowRows * D)); };
+        int i = first;
+        for (; i + step < many; i += 2 * step) {
+            const int64_t x = slot(i), y = slot(i + step);
+            const float2 sx = s.stats[x * 64 + lane], sy = s.stats[y * 64 + lane];
+            const f32x4 (*const fx)[64] = sums(x), (*const fy)[64] = sums(y);
+            f32x4 ox[kDims], oy[kDims];
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) { ox[d] = fx[d][lane]; oy[d] = fy[d][lane]; }
+            const float to = fmaxf(top, fmaxf(sx.x, sy.x)), base = to == -__builtin_inff() ? 0.0f : to;
+            const float mine = __builtin_amdgcn_exp2f(top - base), ex = __builtin_amdgcn_exp2f(sx.x - base), ey = __builtin_amdgcn_exp2f(sy.x - base);
+            top = to;
+            sum = sum * mine + (sx.y * ex + sy.y * ey);
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) o[d] = o[d] * mine + (ox[d] * ex + oy[d] * ey);
+        }
+        if (i < many) { const int64_t x = slot(i); take(s.stats[x * 64 + lane], sums(x), lane); }
     }
 
     __device__ __forceinline__ void clear() {
@@ -350,68 +370,147 @@ struct Narrow {
     }
 };
 
-__device__ __forceinline__ NarrowPart narrow_part(const PagedAttention &a, const Tile &t, int head) {
-    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, t.request);
+__device__ __forceinline__ NarrowPart narrow_part(const PagedAttention &a, const PagedRequest &rq, int request, int row0, int head) {
     NarrowPart p;
-    p.request = t.request;
+    p.request = request;
     p.first_token = rq.first; p.count = rq.count; p.position0 = rq.kv - rq.count;
-    p.row0 = t.row0;
-    p.rows = min(kNarrowRows, rq.count * a.q.group - t.row0);
+    p.row0 = row0;
+    p.rows = min(kNarrowRows, rq.count * a.q.group - row0);
     p.head = head;
-    const int see = p.position0 + (t.row0 + p.rows - 1) / a.q.group + 1;
+    const int see = p.position0 + (row0 + p.rows - 1) / a.q.group + 1;
     p.subs = max(0, (see + 15) / 16);
     return p;
 }
 
+// Where the workers' shares begin and end, for few requests: every wavefront counts the tiles and units itself, a request to a lane, instead
+// of reading them from another kernel's arrays.
+struct Counted {
+    const PagedAttention *a;
+    int64_t per_head;                   // units
+    int tiles, units;                   // of the lane's request, of the last 64 that were counted
+    int64_t upto;                       // units of the requests up to it
+
+    __device__ __forceinline__ void count(int base, int64_t before) {
+        const int r = base + ((int)threadIdx.x & 63);
+        tiles = 0;
+        int64_t u = 0;
+        if (r < a->req.n_requests) {
+            const PagedRequest rq = paged_request(a->req, a->cache.page_shift, r);
+            tiles = (rq.count * a->q.group + kNarrowRows - 1) / kNarrowRows;
+            for (int i = 0; i < tiles; ++i) u += tile_units(rq, a->q.group, kNarrowRows, kNarrowKeys, i);
+        }
+        int64_t sum = u;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) { const int64_t up = __shfl_up(sum, d); if (((int)threadIdx.x & 63) >= d) sum += up; }
+        units = (int)u;
+        upto = before + sum;
+    }
+    __device__ __forceinline__ explicit Counted(const PagedAttention &args) : a(&args), per_head(0), tiles(0), units(0), upto(0) {
+        for (int base = 0; base < a->req.n_requests; base += 64) { count(base, per_head); per_head = uniform(__shfl(upto, 63)); }
+    }
+};
+
+// A worker's way through the segments.
+struct Cursor {
+    PagedRequest rq;
+    int request, tile, tiles, head;
+    int64_t begin;                      // the segment's first unit
+    __device__ __forceinline__ void enter(const PagedAttention &a, int r) {
+        request = uniform(r);
+        rq = paged_request(a.req, a.cache.page_shift, request);
+        tiles = (rq.count * a.q.group + kNarrowRows - 1) / kNarrowRows;
+        tile = 0;
+    }
+    __device__ __forceinline__ int units(const PagedAttention &a) const { return tile_units(rq, a.q.group, kNarrowRows, kNarrowKeys, tile); }
+    __device__ __forceinline__ void find(Counted &c, const PagedAttention &a, int64_t at) {
+        head = (int)(at / c.per_head);
+        const int64_t x = at - head * c.per_head;
+        int64_t before = 0;
+        for (int base = 0;; base += 64) {
+            if (a.req.n_requests > 64) c.count(base, before);
+            const int64_t to = uniform(__shfl(c.upto, 63));
+            if (x < to || base + 64 >= a.req.n_requests) {
+                const int lane = (int)__builtin_ctzll(__ballot(c.upto > x));
+                begin = head * c.per_head + (lane ? uniform(__shfl(c.upto, lane - 1)) : before);
+                enter(a, base + lane);
+                break;
+            }
+            before = to;
+        }
+        for (int u = units(a); at >= begin + u; u = units(a)) { begin += u; ++tile; }
+    }
+    __device__ __forceinline__ void next(const PagedAttention &a, int units) {
+        begin += units;
+        if (++tile < tiles) return;
+        int r = request;
+        do { if (++r == a.req.n_requests) { r = 0; ++head; } enter(a, r); } while (tiles == 0);
+    }
+};
+
+// What a worker does at the least: parts of one unit would cost more to join than they save.
+constexpr int64_t kNarrowLeast = 2;
+
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(const PagedAttention a, const Schedule s) {
     __shared__ __align__(16) half_t<T> s_v[kNarrowWaves][kNarrowKeys * D];
-    const int wave = uniform((int)threadIdx.x >> 6), n_tiles = s.n_tiles[0];
-    if (n_tiles == 0) return;
-    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads;
-    const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves, 1);
+    const int wave = uniform((int)threadIdx.x >> 6);
+    Counted counted(a);
+    const int64_t all = counted.per_head * a.cache.kv_heads;
+    const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves, kNarrowLeast);
     // neighbours in the units' order share an XCD and its L2 (workgroups go to the XCDs in turn)
     const int64_t group = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = group * kNarrowWaves + wave;
     if (w >= workers) return;
     int64_t at = share_begin(all, workers, w);
     const int64_t end = share_begin(all, workers, w + 1);
-    Place place = find_place(s, n_tiles, per_head, at);
-    while (at < end) {
-        const Tile t = s.tiles[place.tile];
-        NarrowPart p = narrow_part(a, Tile{uniform(t.request), uniform(t.row0), uniform(t.units), 0}, place.head);
-        p.unit0 = (int)(at - place.segment_begin);
-        p.unit1 = (int)min((int64_t)t.units, end - place.segment_begin);
-        p.unit0 = uniform(p.unit0); p.unit1 = uniform(p.unit1);
+    if (at == end) return;
+    Cursor c;
+    c.find(counted, a, at);
+    for (;;) {
+        const int units = c.units(a);
+        NarrowPart p = narrow_part(a, c.rq, c.request, c.tile * kNarrowRows, c.head);
+        p.unit0 = uniform((int)(at - c.begin));
+        p.unit1 = uniform((int)min((int64_t)units, end - c.begin));
         Narrow<T, D, false> n;
         n.walk(a, p, s_v[wave]);
-        if (p.unit0 == 0 && p.unit1 == t.units) n.write(a, p);
+        if (p.unit0 == 0 && p.unit1 == units) n.write(a, p);
         else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
-        at = place.segment_begin + p.unit1;
-        if (p.unit1 == t.units) {
-            place.segment_begin = at;
-            if (++place.tile == n_tiles) { place.tile = 0; ++place.head; }
-        }
+        at = c.begin + p.unit1;
+        if (at >= end) break;
+        c.next(a, units);
     }
 }
 
-// The first worker that begins inside a segment joins the segment's parts.
+// The first worker that begins inside a segment joins the segment's parts: its wavefronts take them in turn, then each other's.
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(64) spd_paged_narrow_join_kernel(const PagedAttention a, const Schedule s, const int most_workers) {
-    const int n_tiles = s.n_tiles[0];
-    if (n_tiles == 0) return;
-    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads, workers = workers_for(all, most_workers, 1);
+__global__ void __launch_bounds__(kNarrowWaves * 64) spd_paged_narrow_join_kernel(const PagedAttention a, const Schedule s, const int most_workers) {
+    __shared__ __align__(16) f32x4 s_o[kNarrowWaves - 1][D / 16][64];
+    __shared__ float2 s_stats[kNarrowWaves - 1][64];
+    const int wave = uniform((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+    Counted counted(a);
+    const int64_t all = counted.per_head * a.cache.kv_heads, workers = workers_for(all, most_workers, kNarrowLeast);
     const int64_t w = (int64_t)blockIdx.x + 1;
     if (w >= workers) return;
     const int64_t at = share_begin(all, workers, w);
-    const Place place = find_place(s, n_tiles, per_head, at);
-    if (at == place.segment_begin || share_begin(all, workers, w - 1) > place.segment_begin) return;
-    const Tile t = s.tiles[place.tile];
-    const int64_t end = place.segment_begin + t.units;
+    Cursor c;
+    c.find(counted, a, at);
+    if (at == c.begin || share_begin(all, workers, w - 1) > c.begin) return;
+    const int64_t end = c.begin + c.units(a);
+    int64_t last = w;                   // the last worker with a part
+    while (last + 1 < workers && share_begin(all, workers, last + 1) < end) ++last;
     Narrow<T, D, false> n;
     n.clear();
-    n.join(s, 2 * (w - 1) + 1);
-    for (int64_t other = w; other < workers && share_begin(all, workers, other) < end; ++other) n.join(s, 2 * other);
-    n.write(a, narrow_part(a, t, place.head));
+    const int many = (int)(last - w) + 2;
+    n.join_all(s, many, wave, kNarrowWaves, [&](int i) { return i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1); });
+    if (wave > 0) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) s_o[wave - 1][d][lane] = n.o[d];
+        s_stats[wave - 1][lane] = make_float2(n.top, n.sum);
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int i = 0; i < kNarrowWaves - 1; ++i) n.take(s_stats[i][lane], s_o[i], lane);
+    n.write(a, narrow_part(a, c.rq, c.request, c.tile * kNarrowRows, c.head));
 }
 
 // Selected pages: a segment is a token, a key head and 16 of its query heads, cut into `splits` equal parts.
@@ -450,7 +549,7 @@ __global__ void __launch_bounds__(JOIN ? 64 : kNarrowWaves * 64, JOIN ? 1 : 2)
     Narrow<T, D, true> n;
     if (JOIN) {
         n.clear();
-        for (int i = 0; i < splits; ++i) if (share_begin(units, splits, i + 1) > share_begin(units, splits, i)) n.join(s, segment * splits + i);
+        n.join_all(s, min(units, splits), 0, 1, [&](int i) { return segment * splits + i; });
         n.write(a, p);
         return;
     }
@@ -752,7 +851,8 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
         c.workers = 0;
         return c;
     }
-    c.wide = rows > 24 * (int64_t)a.req.n_requests;
+    // (a wavefront of the narrow kernel counts 64 requests at a time)
+    c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256;
     c.rows = c.wide ? kWideRows : kNarrowRows;
     c.keys = c.wide ? kWideKeys : kNarrowKeys;
     c.threads = c.wide ? kWideWaves * 64 : 64;
@@ -793,13 +893,13 @@ hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Sc
             hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, true>), dim3((unsigned)segments), dim3(64), 0, st, a, s, c.splits, c.head_tiles);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(spd_paged_schedule_kernel, dim3(1), dim3(kScheduleThreads), 0, st, a.req, a.cache.page_shift, a.q.group, c.rows, c.keys, s);
     if (c.wide) {
+        hipLaunchKernelGGL(spd_paged_schedule_kernel, dim3(1), dim3(kScheduleThreads), 0, st, a.req, a.cache.page_shift, a.q.group, c.rows, c.keys, s);
         hipLaunchKernelGGL((spd_paged_wide_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s);
         hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s, c.workers);
     } else {
         hipLaunchKernelGGL((spd_paged_narrow_kernel<T, D>), dim3((unsigned)(c.workers / kNarrowWaves)), dim3(kNarrowWaves * 64), 0, st, a, s);
-        hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(64), 0, st, a, s, c.workers);
+        hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kNarrowWaves * 64), 0, st, a, s, c.workers);
     }
     return hipGetLastError();
 }

@@ -1,4 +1,4 @@
-// The pages that each token and key head attends to: their scores, and the greatest of them.
+// The pages that each token and key head attends to: the scores of all that it sees, and the greatest of them.
 #include <algorithm>
 
 #include "spd_paged_device.h"
@@ -7,127 +7,252 @@ namespace spd {
 
 namespace {
 
-constexpr int kSelectThreads = 256;
+constexpr int kSelectTokens = 16;                                 // to a workgroup, a wavefront to one of them
+constexpr int kSelectThreads = kSelectTokens * 64;
+constexpr int kSelectPages = 2048;                                // of a workgroup: 128 KB of scores
+constexpr int kSelectEach = kSelectPages / 64 + 1;                // of a lane
 
-// A workgroup has one token and key head: its queries as 8-bit codes in LDS, then a page to a thread, scores in scratch, and
-// the greatest one n_select times.
+// Order-preserving whole numbers of scores: greater scores have greater keys.  0 is no page's.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t b = __float_as_uint(x);
+    if (x != x) return 1;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t kForced = 0xffffffffu, kAbsent = 2;
+
+// A wavefront chooses the `k` greatest of `n` keys, equal ones by the lower number, and hands each to `take(rank, number)`, rank
+// ascending with the number.  Lane l holds the numbers l * each .. + each - 1, each <= kSelectEach.  The k-th key is found bit by bit: the keys at
+// or above a candidate are counted with a ballot to a register, and the search ends as soon as a candidate leaves k.
+template <typename Key, typename Take>
+__device__ __forceinline__ void choose(int n, int k, int each, Key key, Take take) {
+    const int lane = (int)threadIdx.x & 63, first = lane * each;
+    uint32_t mine[kSelectEach];
+#pragma unroll
+    for (int j = 0; j < kSelectEach; ++j) {
+        mine[j] = 0;
+        if (j < each && first + j < n) mine[j] = key(first + j);
+    }
+    uint32_t floor = 0;
+    bool exact = false;                                           // as many as k lie at or above `floor`
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const uint32_t to = floor | 1u << bit;
+        int count = 0;
+#pragma unroll
+        for (int j = 0; j < kSelectEach; ++j) if (j < each) count += __popcll(__ballot(mine[j] >= to));
+        if (count >= k) floor = to;
+        exact = count == k;
+    }
+    // those above the floor, and of those at it as many as are left, lower numbers first
+    int above = 0, at = 0;
+#pragma unroll
+    for (int j = 0; j < kSelectEach; ++j) if (j < each) { above += mine[j] > floor; at += mine[j] == floor && floor > 0; }
+    int both = above | at << 16, sum = both;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { const int up = __shfl_up(sum, d); if (lane >= d) sum += up; }
+    const int all = __shfl(sum, 63), left = k - (all & 0xffff);
+    int before_above = (sum - both) & 0xffff, before_at = (sum - both) >> 16;
+#pragma unroll
+    for (int j = 0; j < kSelectEach; ++j) {
+        if (j < each) {
+            const bool is_at = mine[j] == floor && floor > 0;
+            if (mine[j] > floor || (is_at && before_at < left)) take(before_above + min(before_at, left), first + j);
+            before_above += mine[j] > floor;
+            before_at += is_at;
+        }
+    }
+}
+
+struct Candidate { uint32_t key; int32_t page; };
+
+// A tile of tokens: workgroups `b` < blocks have the tokens from 16 b to the end of the block or of the request that 16 b is in, the others
+// the first tokens of request b - blocks, where it begins inside a block.
+struct TokenTile { int request, first, count; };
+__device__ __forceinline__ TokenTile token_tile(const PagedRequests &req, int b, int blocks) {
+    TokenTile t{-1, 0, 0};
+    if (b < blocks) {
+        t.first = b * kSelectTokens;
+        t.request = paged_request_of(req, t.first);
+    } else {
+        t.request = b - blocks;
+        t.first = max(req.query_start[t.request], 0);
+        if (t.first % kSelectTokens == 0) t.request = -1;
+    }
+    if (t.request < 0) return t;
+    const int end = min(min(max(req.query_start[t.request + 1], 0), req.n_tokens), (t.first / kSelectTokens + 1) * kSelectTokens);
+    t.count = max(0, end - t.first);
+    return t;
+}
+
+// Up to 16 tokens of a request against up to 2,048 of its pages, in one key head.  Both sides' 8-bit codes go through the matrix
+// units, 16 pages by 16 tokens, (-w, u) against (lo, hi); a wavefront takes 16 pages a step, so the codes are read
+// once for all tokens of the workgroup.  The scores stay in LDS as keys, and a wavefront chooses for each token.  Where a
+// request has more pages, every 2,048 give their n_select best, and spd_paged_select_join_kernel chooses among those.
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const PagedAttention a, int32_t *const selected, float *const scores,
-                                                                           const int t0) {
+__global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const PagedAttention a, int32_t *const selected, Candidate *const candidates,
+                                                                           const int blocks, const int room) {
     using H = half_t<T>;
-    __shared__ __align__(16) int8_t s_code[2][D];                 // u, then w
-    __shared__ float s_most[4];
-    __shared__ uint64_t s_best[4];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, t = t0 + (int)blockIdx.x, kvh = (int)blockIdx.y, group = a.q.group;
+    constexpr int kSteps = 2 * D / 64, E = D / 64;
+    extern __shared__ __align__(16) uint32_t s_key[];             // [16][room]
+    __shared__ __align__(16) int8_t s_code[kSelectTokens][2 * D];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kvh = (int)blockIdx.y, group = a.q.group, chunk = (int)blockIdx.z;
+    const TokenTile tile = token_tile(a.req, (int)blockIdx.x, blocks);
+    if (tile.count == 0) return;
+    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, tile.request);
+    const int position0 = rq.kv - rq.count + tile.first - rq.first, shift = a.cache.page_shift;
+    const int page0 = chunk * kSelectPages, most = position0 + tile.count - 1 < 0 ? 0 : ((position0 + tile.count - 1) >> shift) + 1;     // pages that the last token sees
+    if (page0 > 0 && page0 >= most) return;
+    const int pages = min(most - page0, kSelectPages);            // of this workgroup
+    if (most > a.n_select) {
+        if (wave < tile.count) {
+            const H *const q = (const H *)a.q.ptr + (int64_t)(tile.first + wave) * a.q.token_stride + (int64_t)kvh * group * a.q.head_stride + lane * E;
+            float big = 0.0f;
+            for (int g = 0; g < group; ++g)
+#pragma unroll
+                for (int e = 0; e < E; ++e) big = fmaxf(big, fabsf((float)q[g * a.q.head_stride + e]));
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
+            const float step = big * kPagedCodeStep, share = 1.0f / (float)group;
+            int up[E], down[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) up[e] = down[e] = 0;
+            for (int g = 0; g < group; ++g)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int c = step > 0.0f ? (int)rintf((float)q[g * a.q.head_stride + e] / step) : 0;
+                    up[e] += max(c, 0); down[e] += max(-c, 0);
+                }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                s_code[wave][lane * E + e] = (int8_t)-(int)rintf((float)down[e] * share);
+                s_code[wave][D + lane * E + e] = (int8_t)rintf((float)up[e] * share);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2 * E; ++e) s_code[wave][lane * 2 * E + e] = 0;
+        }
+        __syncthreads();
+        const int low = lane & 15, quad = lane >> 4;
+        i32x4 q[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = *(const i32x4 *)&s_code[low][s * 64 + quad * 16];
+        const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride + page0;
+        const int own = low < tile.count && position0 + low >= 0 ? (position0 + low) >> shift : -1;    // of token `low`
+        for (int p0 = wave * 16; p0 < pages; p0 += kSelectTokens * 16) {
+            const int32_t number = p0 + low < pages ? table[p0 + low] : -1;
+            const bool there = number >= 0 && number < a.cache.n_pages;
+            const int64_t at = (int64_t)(there ? number : 0) * a.cache.kv_heads + kvh;
+            i32x4 c[kSteps];
+            float scale = -__builtin_inff();                      // (marks a page that is not there)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) c[s] = i32x4{0, 0, 0, 0};
+            if (there) {
+                const int8_t *const from = a.cache.codes + at * 2 * D + quad * 16;
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) c[s] = *(const i32x4 *)(from + s * 64);
+                scale = a.cache.code_scale[at];
+            }
+            i32x4 x = {0, 0, 0, 0};
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_i32_16x16x64_i8(c[s], q[s], x, 0, 0, 0);
+            uint32_t key[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float of_page = __shfl(scale, quad * 4 + i);
+                const int p = page0 + p0 + quad * 4 + i;
+                key[i] = of_page == -__builtin_inff() ? kAbsent : key_of((float)x[i] * of_page);
+                if (p == 0 || p == own) key[i] = kForced;
+                if (p > own) key[i] = 0;
+            }
+            *(uint4 *)&s_key[low * room + p0 + quad * 4] = make_uint4(key[0], key[1], key[2], key[3]);
+        }
+        __syncthreads();
+    }
+    if (wave >= tile.count) return;
+    const int t = tile.first + wave, position = position0 + wave, sees = position < 0 ? 0 : (position >> shift) + 1, k = a.n_select;
+    int32_t *const out = selected + ((int64_t)t * a.cache.kv_heads + kvh) * k;
+    if (sees <= k) {
+        if (chunk == 0 && lane < k) out[lane] = lane < sees ? lane : -1;
+        return;
+    }
+    const int n = min(sees - page0, kSelectPages);
+    if (n <= 0) return;
+    const int each = min((n + 63) / 64 | 1, kSelectEach);         // (odd: lanes read different banks)
+    const uint32_t *const keys = s_key + wave * room;
+    const auto key = [&](int i) { return keys[i]; };
+    if (sees <= kSelectPages) {
+        choose(n, k, each, key, [&](int rank, int i) { out[rank] = i; });
+        return;
+    }
+    Candidate *const to = candidates + (((int64_t)t * a.cache.kv_heads + kvh) * gridDim.z + chunk) * k;
+    if (n < k && lane >= n && lane < k) to[lane] = Candidate{0, -1};
+    choose(n, min(n, k), each, key, [&](int rank, int i) { to[rank] = Candidate{keys[i], page0 + i}; });
+}
+
+// A wavefront to a token and key head of more than 2,048 pages: the best of the lists of each 2,048, as many lists at a time as lanes have room for.
+__global__ void __launch_bounds__(64) spd_paged_select_join_kernel(const PagedAttention a, int32_t *const selected, Candidate *const candidates,
+                                                                    const int chunks) {
+    const int lane = (int)threadIdx.x & 63, t = (int)blockIdx.x, kvh = (int)blockIdx.y, k = a.n_select;
     const int r = paged_request_of(a.req, t);
     if (r < 0) return;
     const PagedRequest rq = paged_request(a.req, a.cache.page_shift, r);
-    const int position = rq.kv - rq.count + (t - rq.first);
-    int32_t *const out = selected + ((int64_t)t * a.cache.kv_heads + kvh) * a.n_select;
-    const int pages = position < 0 ? 0 : (position >> a.cache.page_shift) + 1;
-    if (pages <= a.n_select) {
-        if (tid < a.n_select) out[tid] = tid < pages ? tid : -1;
-        return;
-    }
-    const H *const q = (const H *)a.q.ptr + t * a.q.token_stride + (int64_t)kvh * group * a.q.head_stride;
-    float most = 0.0f;
-    for (int i = tid; i < group * D; i += kSelectThreads) most = fmaxf(most, fabsf((float)q[(i / D) * a.q.head_stride + i % D]));
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    if (lane == 0) s_most[wave] = most;
-    __syncthreads();
-    const float step = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3])) * kPagedCodeStep;
-    if (tid < D) {
-        int up = 0, down = 0;
-        for (int g = 0; g < group; ++g) {
-            const int c = step > 0.0f ? (int)rintf((float)q[g * a.q.head_stride + tid] / step) : 0;
-            up += max(c, 0); down += max(-c, 0);
+    const int position = rq.kv - rq.count + (t - rq.first), sees = position < 0 ? 0 : (position >> a.cache.page_shift) + 1;
+    if (sees <= kSelectPages) return;
+    Candidate *const from = candidates + ((int64_t)t * a.cache.kv_heads + kvh) * chunks * k;
+    int32_t *const out = selected + ((int64_t)t * a.cache.kv_heads + kvh) * k;
+    const int lists = (sees + kSelectPages - 1) / kSelectPages, at_once = 64 * kSelectEach / k;
+    __shared__ Candidate s_kept[64];
+    // what is kept so far goes into the first list of the next round
+    for (int l0 = 0; l0 < lists; ) {
+        const int many = min(at_once, lists - l0), n = many * k;
+        const bool last = l0 + many == lists;
+        Candidate *const list = from + (int64_t)l0 * k;
+        Candidate *const next = from + (int64_t)(l0 + many - 1) * k;
+        const int each = min((n + 63) / 64 | 1, kSelectEach);
+        if (last) {
+            choose(n, k, each, [&](int i) { return list[i].key; }, [&](int rank, int i) { out[rank] = list[i].page; });
+            return;
         }
-        const float share = 1.0f / (float)group;
-        s_code[0][tid] = (int8_t)rintf((float)up * share);
-        s_code[1][tid] = (int8_t)rintf((float)down * share);
-    }
-    __syncthreads();
-    float *const score = scores + ((int64_t)blockIdx.x * a.cache.kv_heads + kvh) * a.req.max_pages;
-    const int32_t *const table = a.req.block_table + (int64_t)r * a.req.table_stride;
-    for (int p = tid; p < pages; p += kSelectThreads) {
-        const int32_t number = table[p];
-        float x = -__builtin_inff();
-        if (p == 0 || p == pages - 1) x = __builtin_inff();
-        else if (number >= 0 && number < a.cache.n_pages) {
-            const int64_t at = ((int64_t)number * a.cache.kv_heads + kvh);
-            const int8_t *const c = a.cache.codes + at * 2 * D;
-            int sum = 0;
-            for (int d = 0; d < D; ++d) sum += (int)s_code[0][d] * c[D + d] - (int)s_code[1][d] * c[d];
-            x = (float)sum * a.cache.code_scale[at];
-        }
-        score[p] = x;
-    }
-    // (one workgroup's own stores: a barrier orders them for it)
-    __threadfence_block();
-    __syncthreads();
-    for (int j = 0; j < a.n_select; ++j) {
-        uint64_t best = 0;
-        for (int p = tid; p < pages; p += kSelectThreads) {
-            const uint32_t b = __float_as_uint(score[p]);
-            const uint32_t key = b & 0x80000000u ? ~b : b | 0x80000000u;
-            best = max(best, (uint64_t)key << 32 | (uint32_t)~p);
-        }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) best = max(best, __shfl_xor(best, d));
-        if (lane == 0) s_best[wave] = best;
+        choose(n, k, each, [&](int i) { return list[i].key; }, [&](int rank, int i) { s_kept[rank] = list[i]; });
         __syncthreads();
-        best = max(max(s_best[0], s_best[1]), max(s_best[2], s_best[3]));
-        const int p = (int)~(uint32_t)best;
-        if (tid == 0) { out[j] = p; score[p] = -__builtin_nanf(""); }       // (below every other key)
+        if (lane < k) next[lane] = s_kept[lane];
         __threadfence_block();
         __syncthreads();
+        l0 += many - 1;
     }
-    // ascending: every place's rank among the selected
-    int mine = 0, rank = 0;
-    if (tid < a.n_select) {
-        mine = out[tid];
-        for (int j = 0; j < a.n_select; ++j) rank += out[j] < mine;
-    }
-    __syncthreads();
-    if (tid < a.n_select) out[rank] = mine;
 }
+
+int chunks_of(const PagedAttention &a) { return std::max(1, (a.req.max_pages + kSelectPages - 1) / kSelectPages); }
 
 template <spd_dtype T, int D>
-void start(hipStream_t st, const PagedAttention &a, int32_t *selected, float *scores, int t0, int count) {
-    hipLaunchKernelGGL((spd_paged_select_kernel<T, D>), dim3((unsigned)count, (unsigned)a.cache.kv_heads), dim3(kSelectThreads), 0, st, a,
-                       selected, scores, t0);
-}
-
-constexpr size_t kScoreBytes = (size_t)256 << 20;                 // tokens whose scores take more are scored in several launches
-
-int tokens_at_once(const PagedAttention &a) {
-    const size_t each = std::max<size_t>((size_t)a.cache.kv_heads * (size_t)a.req.max_pages * 4, 1);
-    return (int)std::min<size_t>(std::max<size_t>(kScoreBytes / each, 1), (size_t)std::max(a.req.n_tokens, 1));
+hipError_t start(hipStream_t st, const PagedAttention &a, int32_t *selected, Candidate *candidates) {
+    const int blocks = (a.req.n_tokens + kSelectTokens - 1) / kSelectTokens, chunks = chunks_of(a);
+    const int room = (std::min(a.req.max_pages, kSelectPages) + 15) / 16 * 16 + 4;      // (rows begin 4 banks apart)
+    const size_t lds = (size_t)kSelectTokens * room * 4;
+    const auto kernel = spd_paged_select_kernel<T, D>;
+    if (lds > 48 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks + a.req.n_requests), (unsigned)a.cache.kv_heads, (unsigned)chunks), dim3(kSelectThreads), lds, st,
+                       a, selected, candidates, blocks, room);
+    if (chunks > 1)
+        hipLaunchKernelGGL(spd_paged_select_join_kernel, dim3((unsigned)a.req.n_tokens, (unsigned)a.cache.kv_heads), dim3(64), 0, st, a, selected,
+                           candidates, chunks);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 size_t paged_select_scratch(const PagedAttention &a) {
-    return (size_t)tokens_at_once(a) * (size_t)a.cache.kv_heads * (size_t)a.req.max_pages * 4;
+    const int chunks = chunks_of(a);
+    return chunks > 1 ? (size_t)a.req.n_tokens * (size_t)a.cache.kv_heads * (size_t)chunks * (size_t)a.n_select * sizeof(Candidate) : 0;
 }
 
 hipError_t launch_paged_select(hipStream_t st, const PagedAttention &a, int32_t *selected, void *scratch) {
-    const int each = tokens_at_once(a);
-    for (int t0 = 0; t0 < a.req.n_tokens; t0 += each) {
-        const int count = std::min(each, a.req.n_tokens - t0);
-        float *const scores = static_cast<float *>(scratch);
-        if (a.dtype == SPD_BF16) {
-            if (a.head_dim == 64) start<SPD_BF16, 64>(st, a, selected, scores, t0, count);
-            else start<SPD_BF16, 128>(st, a, selected, scores, t0, count);
-        } else {
-            if (a.head_dim == 64) start<SPD_F16, 64>(st, a, selected, scores, t0, count);
-            else start<SPD_F16, 128>(st, a, selected, scores, t0, count);
-        }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    if (a.req.n_tokens == 0) return hipSuccess;
+    Candidate *const candidates = static_cast<Candidate *>(scratch);
+    if (a.dtype == SPD_BF16) return a.head_dim == 64 ? start<SPD_BF16, 64>(st, a, selected, candidates) : start<SPD_BF16, 128>(st, a, selected, candidates);
+    return a.head_dim == 64 ? start<SPD_F16, 64>(st, a, selected, candidates) : start<SPD_F16, 128>(st, a, selected, candidates);
 }
 
 }  // namespace spd
