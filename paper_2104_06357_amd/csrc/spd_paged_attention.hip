@@ -17,6 +17,7 @@ constexpr float kSlack = 8.0f;          // a row's maximum is moved (and its sum
 // another kernel joins them.
 
 struct Tile { int32_t request, row0, units, pad; };
+struct Joined { int32_t parts, request, first_token, position0, row0, rows, head, pad; };        // parts: 0 if there is no such segment
 struct Schedule {
     int64_t *first;                     // [tiles + 1]: units of the tiles before
     Tile *tiles;
@@ -25,6 +26,7 @@ struct Schedule {
     int64_t most_tiles;                 // room; requests that overlap (which they may not) could have more
     float *sums;                        // [2 * workers][rows of a tile * head_dim] of parts
     float2 *stats;                      // [2 * workers][rows of a tile, as lanes have them]: maximum, sum
+    Joined *joined;                     // [workers]: the segment that a worker began and others went on with
 };
 
 __device__ __forceinline__ int tile_units(const PagedRequest &rq, int group, int rows, int keys, int tile) {
@@ -100,6 +102,12 @@ __device__ __forceinline__ int64_t share_begin(int64_t all, int64_t workers, int
     return all / workers * w + min(w, all % workers);
 }
 
+// The worker who has unit `x`.
+__device__ __forceinline__ int64_t worker_of(int64_t all, int64_t workers, int64_t x) {
+    const int64_t each = all / workers, more = all % workers;
+    return x < (each + 1) * more ? x / (each + 1) : more + (x - (each + 1) * more) / max(each, (int64_t)1);
+}
+
 // As many workers as there are, but no fewer than `least` units to one.
 __device__ __forceinline__ int64_t workers_for(int64_t all, int64_t workers, int64_t least) { return max((int64_t)1, min(workers, all / least)); }
 
@@ -144,8 +152,7 @@ struct Pages {
 
 // ---- few rows: a wavefront to 16 of them --------------------------------------------------------
 // Decoding, and selected pages: one to 16 rows, and every key is read once.  A wavefront is a worker of its own, and no barrier is in its
-// loop: 32 keys a unit, K straight from memory into the first product's operand, V through 8 KB of LDS from where it is
-// read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
+// loop: 32 keys a unit, through 16 KB of LDS, from where V is read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
 // lanes and order in which the second takes them, and a row is a lane's, its statistics too.
 
 constexpr int kNarrowRows = 16, kNarrowKeys = 32, kNarrowWaves = 4;
@@ -163,19 +170,14 @@ struct Narrow {
     using H = half_t<T>;
     using H8 = half8_t<T>;
     static constexpr int kChunks = D / 8;               // 16 bytes each, of a row
-    static constexpr int kSteps = D / 32, kDims = D / 16, kVLoads = kNarrowKeys * kChunks / 64;
-    static constexpr int kRowsOfLoad = 64 / kChunks;    // rows of V in one load of the wavefront
+    static constexpr int kSteps = D / 32, kDims = D / 16, kLoads = kNarrowKeys * kChunks / 64;
+    static constexpr int kRowsOfLoad = 64 / kChunks;    // rows in one load of the wavefront
 
     H8 q[kSteps];
     f32x4 o[kDims];
     float top, sum;
 
-    // where V's chunk c of key row r lies in LDS: rows that are read together in different banks
-    static __device__ __forceinline__ int v_at(int r, int c) {
-        return r * D + (D == 128 ? (c ^ ((r & 3) << 2)) : (c ^ (((r >> 1) & 1) << 2))) * 8;
-    }
-
-    __device__ __forceinline__ void walk(const PagedAttention &a, const NarrowPart &p, H *lds) {
+    __device__ __forceinline__ void walk(const PagedAttention &a, const NarrowPart &p, void *lds) {
         const int lane = (int)threadIdx.x & 63, row = lane & 15, quad = lane >> 4;
         const int f = p.row0 + min(row, p.rows - 1), token = SELECTED ? 0 : f / a.q.group, g = SELECTED ? f : f - token * a.q.group;
         const int position = p.position0 + token;
@@ -201,7 +203,7 @@ struct Narrow {
         } else {
             pages.begin(table, a.req.max_pages, (p.unit0 * 2) >> per_page);
         }
-        H8 kr[2][kSteps], vr[kVLoads];
+        H8 kr[kLoads], vr[kLoads];
         int pos0[2], here[2];                           // of the two 16-key steps: the first key's position, and whether the page is there
         int64_t base[2];
         auto locate = [&](int u, int *pos, int *ok, int64_t *at) {
@@ -216,48 +218,49 @@ struct Narrow {
                 at[j] = (int64_t)number * a.cache.page_stride + (int64_t)in * a.cache.token_stride + (int64_t)p.head * a.cache.head_stride;
             }
         };
-        const int64_t k_lane = (int64_t)row * a.cache.token_stride + quad * 8;
-        const int v_row = lane / kChunks, v_chunk = lane % kChunks;
+        // (a row's chunks go to neighbouring lanes, which memory answers four at a time; the products' order, a row to a lane, is made by LDS)
+        const int l_row = lane / kChunks, l_chunk = lane % kChunks;
+        const uint32_t l_at = (uint32_t)l_row * (uint32_t)a.cache.token_stride * 2 + (uint32_t)l_chunk * 16;
         auto fetch = [&](const int *ok, const int64_t *at) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (!ok[j]) continue;
-                const H *const k = (const H *)a.cache.k + at[j] + k_lane;
+                const char *const k = (const char *)a.cache.k + uniform(at[j]) * 2, *const v = (const char *)a.cache.v + uniform(at[j]) * 2;
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) kr[j][s] = *(const H8 *)(k + s * 32);
-                const H *const v = (const H *)a.cache.v + at[j] + (int64_t)v_row * a.cache.token_stride + v_chunk * 8;
-#pragma unroll
-                for (int i = 0; i < kVLoads / 2; ++i) vr[j * (kVLoads / 2) + i] = *(const H8 *)(v + (int64_t)(i * kRowsOfLoad) * a.cache.token_stride);
+                for (int i = 0; i < kLoads / 2; ++i) {
+                    const int64_t more = (int64_t)(i * kRowsOfLoad) * a.cache.token_stride * 2;
+                    kr[j * (kLoads / 2) + i] = *(const H8 *)(k + more + l_at);
+                    vr[j * (kLoads / 2) + i] = *(const H8 *)(v + more + l_at);
+                }
             }
         };
         H8 zero;
 #pragma unroll
         for (int i = 0; i < 8; ++i) zero[i] = (H)0.0f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) kr[j][s] = zero;
-#pragma unroll
-        for (int i = 0; i < kVLoads; ++i) vr[i] = zero;
+        for (int i = 0; i < kLoads; ++i) kr[i] = vr[i] = zero;
+        const LdsBytes s_k = lds_bytes(lds), s_v = s_k + kNarrowKeys * D * 2;
+        const int s = lane & 15, k_lane = k_at<D>(row, quad), v_lane = v_at<D>(quad * 4 + (s >> 2), (s & 3) >> 1) + (s & 1) * 8;
         locate(p.unit0, pos0, here, base);
         fetch(here, base);
         for (int u = p.unit0; u < p.unit1; ++u) {
             int pos_next[2] = {0, 0}, here_next[2] = {0, 0};
             int64_t base_next[2] = {0, 0};
             if (u + 1 < p.unit1) locate(u + 1, pos_next, here_next, base_next);
-            // V into LDS; what no row of the tile sees becomes 0, since 0 times what lies there need not be
+            // into LDS; values that no row of the tile sees become 0, since 0 times what lies there need not be
 #pragma unroll
-            for (int i = 0; i < kVLoads; ++i) {
-                const int j = i / (kVLoads / 2), r = (i % (kVLoads / 2)) * kRowsOfLoad + v_row;
+            for (int i = 0; i < kLoads; ++i) {
+                const int j = i / (kLoads / 2), r = (i % (kLoads / 2)) * kRowsOfLoad + l_row;
+                write_row<T>(s_k + k_at<D>(j * 16 + r, l_chunk), kr[i]);
                 if (!here[j] || pos0[j] + 15 > most) { if (!here[j] || pos0[j] + r > most) vr[i] = zero; }
-                *(H8 *)(lds + v_at(j * 16 + r, v_chunk)) = vr[i];
+                write_row<T>(s_v + v_at<D>(j * 16 + r, l_chunk), vr[i]);
             }
             f32x4 x[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 x[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) x[j] = mfma16(kr[j][s], q[s], x[j]);
+                for (int s = 0; s < kSteps; ++s) x[j] = mfma16(read_row<T>(s_k + (k_lane ^ (s << 6)) + j * 32 * D), q[s], x[j]);
             }
             const int now_pos[2] = {pos0[0], pos0[1]}, now_here[2] = {here[0], here[1]};
 #pragma unroll
@@ -268,7 +271,7 @@ struct Narrow {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) w[j * 4 + i] = x[j][i] * a.q.scale;
+                for (int i = 0; i < 4; ++i) w[j * 4 + i] = x[j][i];
                 if (!now_here[j] || now_pos[j] + 15 > least)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) if (!now_here[j] || now_pos[j] + quad * 4 + i > position) w[j * 4 + i] = -__builtin_inff();
@@ -277,7 +280,7 @@ struct Narrow {
 #pragma unroll
             for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
             big = fmaxf(big, __shfl_xor(big, 16));
-            big = fmaxf(big, __shfl_xor(big, 32));
+            big = fmaxf(big, __shfl_xor(big, 32)) * a.q.scale;
             if (__any(big > top + kSlack)) {
                 const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
                 top = to;
@@ -287,20 +290,10 @@ struct Narrow {
             }
             const float from = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(w[i] - from); sum += w[i]; }
+            for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(w[i], a.q.scale, -from)); sum += w[i]; }
             const H8 pw = rounded<T>(w);
-            const int s = lane & 15;
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) {
-                half4_t<T> part[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = j * 16 + quad * 4 + (s >> 2);
-                    part[j] = read_transposed<T>(lds + v_at(r, d * 2 + ((s & 3) >> 1)) + (s & 1) * 4);
-                }
-                const H8 v = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                o[d] = mfma16(v, pw, o[d]);
-            }
+            for (int d = 0; d < kDims; ++d) o[d] = mfma16(read_transposed<T>(s_v + (v_lane ^ (d << 5)), 32 * D), pw, o[d]);
         }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
@@ -452,55 +445,48 @@ constexpr int64_t kNarrowLeast = 2;
 
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(const PagedAttention a, const Schedule s) {
-    __shared__ __align__(16) half_t<T> s_v[kNarrowWaves][kNarrowKeys * D];
+    __shared__ __align__(16) half_t<T> s_kv[kNarrowWaves][2 * kNarrowKeys * D];
     const int wave = uniform((int)threadIdx.x >> 6);
     Counted counted(a);
     const int64_t all = counted.per_head * a.cache.kv_heads;
     const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves, kNarrowLeast);
     // neighbours in the units' order share an XCD and its L2 (workgroups go to the XCDs in turn)
     const int64_t group = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = group * kNarrowWaves + wave;
-    if (w >= workers) return;
-    int64_t at = share_begin(all, workers, w);
-    const int64_t end = share_begin(all, workers, w + 1);
-    if (at == end) return;
+    int64_t at = w < workers ? share_begin(all, workers, w) : all;
+    const int64_t end = w < workers ? share_begin(all, workers, w + 1) : all;
+    Joined joined{};
     Cursor c;
-    c.find(counted, a, at);
-    for (;;) {
+    if (at < end) c.find(counted, a, at);
+    while (at < end) {
         const int units = c.units(a);
         NarrowPart p = narrow_part(a, c.rq, c.request, c.tile * kNarrowRows, c.head);
         p.unit0 = uniform((int)(at - c.begin));
         p.unit1 = uniform((int)min((int64_t)units, end - c.begin));
         Narrow<T, D, false> n;
-        n.walk(a, p, s_v[wave]);
+        n.walk(a, p, s_kv[wave]);
         if (p.unit0 == 0 && p.unit1 == units) n.write(a, p);
         else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
+        if (p.unit0 == 0 && p.unit1 < units)
+            joined = Joined{(int)(worker_of(all, workers, c.begin + units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, 0};
         at = c.begin + p.unit1;
-        if (at >= end) break;
-        c.next(a, units);
+        if (at < end) c.next(a, units);
     }
+    if (((int)threadIdx.x & 63) == 0) s.joined[w] = joined;
 }
 
-// The first worker that begins inside a segment joins the segment's parts: its wavefronts take them in turn, then each other's.
+// A workgroup to a worker: the segment that it began and others went on with, if there is one.  The wavefronts take its parts in turn, then
+// each other's.
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kNarrowWaves * 64) spd_paged_narrow_join_kernel(const PagedAttention a, const Schedule s, const int most_workers) {
+__global__ void __launch_bounds__(kNarrowWaves * 64) spd_paged_narrow_join_kernel(const PagedAttention a, const Schedule s) {
     __shared__ __align__(16) f32x4 s_o[kNarrowWaves - 1][D / 16][64];
     __shared__ float2 s_stats[kNarrowWaves - 1][64];
     const int wave = uniform((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
-    Counted counted(a);
-    const int64_t all = counted.per_head * a.cache.kv_heads, workers = workers_for(all, most_workers, kNarrowLeast);
-    const int64_t w = (int64_t)blockIdx.x + 1;
-    if (w >= workers) return;
-    const int64_t at = share_begin(all, workers, w);
-    Cursor c;
-    c.find(counted, a, at);
-    if (at == c.begin || share_begin(all, workers, w - 1) > c.begin) return;
-    const int64_t end = c.begin + c.units(a);
-    int64_t last = w;                   // the last worker with a part
-    while (last + 1 < workers && share_begin(all, workers, last + 1) < end) ++last;
+    const Joined j = s.joined[blockIdx.x];
+    if (j.parts == 0) return;
+    const int64_t w = blockIdx.x;
     Narrow<T, D, false> n;
     n.clear();
-    const int many = (int)(last - w) + 2;
-    n.join_all(s, many, wave, kNarrowWaves, [&](int i) { return i == 0 ? 2 * (w - 1) + 1 : 2 * (w + i - 1); });
+    n.join_all(s, j.parts, wave, kNarrowWaves, [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); });
     if (wave > 0) {
 #pragma unroll
         for (int d = 0; d < D / 16; ++d) s_o[wave - 1][d][lane] = n.o[d];
@@ -510,14 +496,16 @@ __global__ void __launch_bounds__(kNarrowWaves * 64) spd_paged_narrow_join_kerne
     if (wave > 0) return;
 #pragma unroll
     for (int i = 0; i < kNarrowWaves - 1; ++i) n.take(s_stats[i][lane], s_o[i], lane);
-    n.write(a, narrow_part(a, c.rq, c.request, c.tile * kNarrowRows, c.head));
+    NarrowPart p{};
+    p.first_token = j.first_token; p.row0 = j.row0; p.rows = j.rows; p.head = j.head;
+    n.write(a, p);
 }
 
 // Selected pages: a segment is a token, a key head and 16 of its query heads, cut into `splits` equal parts.
 template <spd_dtype T, int D, bool JOIN>
 __global__ void __launch_bounds__(JOIN ? 64 : kNarrowWaves * 64, JOIN ? 1 : 2)
     spd_paged_selected_kernel(const PagedAttention a, const Schedule s, const int splits, const int head_tiles) {
-    __shared__ __align__(16) half_t<T> s_v[JOIN ? 1 : kNarrowWaves][JOIN ? 8 : kNarrowKeys * D];
+    __shared__ __align__(16) half_t<T> s_kv[JOIN ? 1 : kNarrowWaves][JOIN ? 8 : 2 * kNarrowKeys * D];
     const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     // (a token's and its neighbours' segments share pages: neighbours share an XCD)
     const int64_t blocks = (int64_t)gridDim.x, per = blocks / 8, rest = blocks % 8, xcd = blockIdx.x % 8;
@@ -530,9 +518,9 @@ __global__ void __launch_bounds__(JOIN ? 64 : kNarrowWaves * 64, JOIN ? 1 : 2)
     const int tile = (int)(segment % head_tiles);
     const int64_t rest_of = segment / head_tiles;
     const int token = (int)(rest_of % a.req.n_tokens), head = (int)(rest_of / a.req.n_tokens);
-    const int r = paged_request_of(a.req, token);
+    PagedRequest rq;
+    const int r = paged_request_of(a.req, a.cache.page_shift, uniform(token), rq);
     if (r < 0) return;
-    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, r);
     NarrowPart p;
     p.request = uniform(r);
     p.first_token = uniform(token); p.count = 1;
@@ -556,13 +544,13 @@ __global__ void __launch_bounds__(JOIN ? 64 : kNarrowWaves * 64, JOIN ? 1 : 2)
     p.unit0 = uniform((int)share_begin(units, splits, split));
     p.unit1 = uniform((int)share_begin(units, splits, split + 1));
     if (p.unit0 == p.unit1) return;
-    n.walk(a, p, s_v[JOIN ? 0 : wave]);
+    n.walk(a, p, s_kv[JOIN ? 0 : wave]);
     if (splits == 1) n.write(a, p); else n.leave(s, w);
 }
 
-// ---- many rows: a workgroup to 128 of them -------------------------------------------------------
+// ---- many rows: a workgroup to 256 of them -------------------------------------------------------
 
-constexpr int kWideRows = 128, kWideKeys = 64, kWideWaves = 4;
+constexpr int kWideRows = 256, kWideKeys = 64, kWideWaves = 8;
 
 struct WidePart {
     int request, first_token, position0, row0, rows, head;
@@ -575,17 +563,12 @@ struct Wide {
     using H = half_t<T>;
     using H8 = half8_t<T>;
     static constexpr int kChunks = D / 8, kSteps = D / 16, kDims = D / 32;
-    static constexpr int kRowsOfLoad = kWideWaves * 64 / kChunks, kLoads = kWideKeys / kRowsOfLoad;
-    static constexpr int kTile = kWideKeys * D;         // values of K or V in LDS
+    static constexpr int kThreads = kWideWaves * 64, kRowsOfLoad = kThreads / kChunks, kLoads = kWideKeys / kRowsOfLoad;
+    static constexpr int kTile = kWideKeys * D * 2;     // bytes of K or V in LDS
 
     H8 q[kSteps];
     f32x16 o[kDims];
     float top, sum;
-
-    static __device__ __forceinline__ int k_at(int r, int c) { return r * D + (D == 128 ? (c ^ (r & 15)) : (c ^ ((r >> 1) & 7))) * 8; }
-    static __device__ __forceinline__ int v_at(int r, int c) {
-        return r * D + (D == 128 ? (c ^ ((r & 3) << 2)) : (c ^ (((r >> 1) & 1) << 2))) * 8;
-    }
 
     __device__ __forceinline__ void clear() {
         top = -__builtin_inff(); sum = 0.0f;
@@ -596,7 +579,7 @@ struct Wide {
     }
 
     // lds: two buffers of K and V
-    __device__ __forceinline__ void walk(const PagedAttention &a, const WidePart &p, H *lds) {
+    __device__ __forceinline__ void walk(const PagedAttention &a, const WidePart &p, void *lds) {
         const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), half = lane >> 5;
         const int mine = wave * 32 + (lane & 31), f = p.row0 + min(mine, p.rows - 1), token = f / a.q.group, g = f - token * a.q.group;
         const int position = p.position0 + token;
@@ -614,110 +597,117 @@ struct Wide {
         Pages pages;
         pages.begin(a.req.block_table + (int64_t)p.request * a.req.table_stride, a.req.max_pages, (p.unit0 * kWideKeys) >> shift);
         const int l_row = tid / kChunks, l_chunk = tid % kChunks;
-        H8 kr[kLoads], vr[kLoads];
-        uint64_t there = 0, there_next;                 // keys of the unit whose page is there
+        const uint32_t l_at = (uint32_t)(l_row & 15) * (uint32_t)a.cache.token_stride * 2 + (uint32_t)l_chunk * 16;
         H8 zero;
 #pragma unroll
         for (int i = 0; i < 8; ++i) zero[i] = (H)0.0f;
-        auto fetch = [&](int u) {
-            there_next = 0;
+        struct Loaded { H8 k[kLoads], v[kLoads]; uint64_t there; };     // of a unit; there: keys whose page is there
+        auto fetch = [&](int u, Loaded &to) {
+            to.there = 0;
             int number[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {               // 16 keys lie in one page
-                const int i = (u * kWideKeys + j * 16) >> shift;
-                number[j] = pages.number(i);
-                const bool ok = number[j] >= 0 && number[j] < a.cache.n_pages && u * kWideKeys + j * 16 < p.see;
-                there_next |= ok ? 0xffffull << (16 * j) : 0;
+                const int key = u * kWideKeys + j * 16;
+                number[j] = pages.number(key >> shift);
+                to.there |= number[j] >= 0 && number[j] < a.cache.n_pages && key < p.see ? 0xffffull << (16 * j) : 0;
             }
+            const bool whole = to.there == ~0ull && (u + 1) * kWideKeys <= p.see;
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
-                const int r = l * kRowsOfLoad + l_row, key = u * kWideKeys + r;
-                int j = 0, which = number[0];
-                if (D == 128) { j = l; which = number[l]; }
-                else { j = 2 * l + (wave >> 1); which = wave >> 1 ? number[2 * l + 1 < 4 ? 2 * l + 1 : 3] : number[2 * l < 4 ? 2 * l : 3]; }
-                const bool ok = (there_next >> (16 * j)) & 1;
-                kr[l] = zero; vr[l] = zero;
-                if (ok && key < p.see) {
-                    const int64_t at = (int64_t)which * a.cache.page_stride + (int64_t)(key & ((1 << shift) - 1)) * a.cache.token_stride +
-                                       (int64_t)p.head * a.cache.head_stride + l_chunk * 8;
-                    kr[l] = *(const H8 *)((const H *)a.cache.k + at);
-                    vr[l] = *(const H8 *)((const H *)a.cache.v + at);
+                const int j = uniform((l * kRowsOfLoad + wave * (64 / kChunks)) / 16), key = u * kWideKeys + j * 16;      // the wavefront's rows of this load
+                const int which = uniform(j == 0 ? number[0] : j == 1 ? number[1] : j == 2 ? number[2] : number[3]);
+                const int64_t at = uniform(((int64_t)which * a.cache.page_stride + (int64_t)(key & ((1 << shift) - 1)) * a.cache.token_stride +
+                                            (int64_t)p.head * a.cache.head_stride) * 2);
+                const bool seen = whole || (((to.there >> (16 * j)) & 1) && key + (l_row & 15) < p.see);
+                if (!whole) { to.k[l] = zero; to.v[l] = zero; }
+                if (seen) {
+                    to.k[l] = *(const H8 *)((const char *)a.cache.k + at + l_at);
+                    to.v[l] = *(const H8 *)((const char *)a.cache.v + at + l_at);
                 }
             }
         };
-        auto store = [&](int buffer) {
-            H *const k = lds + buffer * 2 * kTile, *const v = k + kTile;
+        const LdsBytes kv = lds_bytes(lds);
+        const int k_to = k_at<D>(l_row, l_chunk), v_to = v_at<D>(l_row, l_chunk) + kTile;
+        auto store = [&](int buffer, const Loaded &from) {
+            const LdsBytes k = kv + buffer * 2 * kTile;
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) {
-                const int r = l * kRowsOfLoad + l_row;
-                *(H8 *)(k + k_at(r, l_chunk)) = kr[l];
-                *(H8 *)(v + v_at(r, l_chunk)) = vr[l];
+            for (int l = 0; l < kLoads; ++l) {          // (the rows of a load differ from the first's in no bit that the layout looks at)
+                write_row<T>(k + k_to + l * kRowsOfLoad * D * 2, from.k[l]);
+                write_row<T>(k + v_to + l * kRowsOfLoad * D * 2, from.v[l]);
             }
         };
-        fetch(p.unit0);
-        there = there_next;
-        store(0);
+        // K Q^T, a column to a lane: keys 32 t + 8 (i / 4) + 4 half + i % 4; then the softmax's weights, and V^T times them.  `edge`: some key
+        // is not to be seen by some row.
+        const int s16 = lane & 15, k_lane = k_at<D>(lane & 31, half),
+                  v_lane = v_at<D>(half * 4 + (s16 >> 2), ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8 + kTile;
+        auto attend = [&](const LdsBytes k, int key0, uint64_t there) {
+            if (!busy || key0 > most) return;
+            const bool edge = key0 + kWideKeys - 1 > least || there != ~0ull;
+            f32x16 x[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) x[t] = mfma32(read_row<T>(k + (k_lane ^ (s << 5)) + t * 64 * D), q[s], x[t]);
+            if (edge) {
+                asm volatile("");                       // (a branch: few units have one)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const int c = (i >> 4) * 32 + ((i & 15) >> 2) * 8 + half * 4 + (i & 3);
+                    if (key0 + c > position || !((there >> c) & 1)) x[i >> 4][i & 15] = -__builtin_inff();
+                }
+            }
+            float big = x[0][0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) big = fmaxf(big, x[i >> 4][i & 15]);
+            big = fmaxf(big, __shfl_xor(big, 32)) * a.q.scale;
+            if (__any(big > top + kSlack)) {
+                const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+                top = to;
+                sum *= old;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[d][i] *= old;
+            }
+            const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {               // 16 keys
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(x[e >> 1][(e & 1) * 8 + i], a.q.scale, -from)); sum += w[i]; }
+                const H8 pw = rounded<T>(w);
+#pragma unroll
+                for (int d = 0; d < kDims; ++d)
+                    o[d] = mfma32(read_transposed<T>(k + (v_lane ^ (d << 6)) + e * 32 * D, 16 * D), pw, o[d]);
+            }
+        };
+        // Unit u is in LDS while u + 1 and u + 2 are on their way in registers: memory has the time of two units to answer.
+        Loaded odd, even;
+        int u = p.unit0;
+        fetch(u, even);
+        if (u + 1 < p.unit1) fetch(u + 1, odd);
+        store(0, even);
+        uint64_t there = even.there;
         __syncthreads();
-        for (int u = p.unit0; u < p.unit1; ++u) {
-            const int buffer = (u - p.unit0) & 1;
-            const bool more = u + 1 < p.unit1;
-            if (more) fetch(u + 1);
-            const int key0 = u * kWideKeys;
-            if (busy && key0 <= most) {
-                const H *const k = lds + buffer * 2 * kTile, *const v = k + kTile;
-                f32x16 x[2];
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[t][i] = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < kSteps; ++s) x[t] = mfma32(*(const H8 *)(k + k_at(t * 32 + (lane & 31), 2 * s + half)), q[s], x[t]);
-                }
-                float w[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) w[i] = x[i >> 4][i & 15] * a.q.scale;
-                if (key0 + kWideKeys - 1 > least || there != ~0ull) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int c = (i >> 4) * 32 + ((i & 15) >> 2) * 8 + half * 4 + (i & 3);
-                        if (key0 + c > position || !((there >> c) & 1)) w[i] = -__builtin_inff();
-                    }
-                }
-                float big = w[0];
-#pragma unroll
-                for (int i = 1; i < 32; ++i) big = fmaxf(big, w[i]);
-                big = fmaxf(big, __shfl_xor(big, 32));
-                if (__any(big > top + kSlack)) {
-                    const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
-                    top = to;
-                    sum *= old;
-#pragma unroll
-                    for (int d = 0; d < kDims; ++d)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] *= old;
-                }
-                const float from = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) { w[i] = __builtin_amdgcn_exp2f(w[i] - from); sum += w[i]; }
-                const int s = lane & 15;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {           // 16 keys
-                    const H8 pw = rounded<T>(w + e * 8);
-#pragma unroll
-                    for (int d = 0; d < kDims; ++d) {
-                        half4_t<T> part[2];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int r = e * 16 + j * 8 + half * 4 + (s >> 2);
-                            part[j] = read_transposed<T>(v + v_at(r, d * 4 + ((lane >> 4) & 1) * 2 + ((s & 3) >> 1)) + (s & 1) * 4);
-                        }
-                        o[d] = mfma32(__builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7), pw, o[d]);
-                    }
-                }
-            }
-            if (more) { store(buffer ^ 1); there = there_next; }
+        for (;;) {
+            if (u + 2 < p.unit1) fetch(u + 2, even);
+            attend(kv, u * kWideKeys, there);
+            if (u + 1 == p.unit1) break;
+            store(1, odd);
+            there = odd.there;
             __syncthreads();
+            ++u;
+            if (u + 2 < p.unit1) fetch(u + 2, odd);
+            attend(kv + 2 * kTile, u * kWideKeys, there);
+            if (u + 1 == p.unit1) break;
+            store(0, even);
+            there = even.there;
+            __syncthreads();
+            ++u;
         }
+        __syncthreads();                                // (the next segment's first unit goes where this one's last may be)
         sum += __shfl_xor(sum, 32);
     }
 
@@ -745,13 +735,13 @@ struct Wide {
 #pragma unroll
         for (int d = 0; d < kDims; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) to[(d * 4 + i) * 256 + tid] = f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
-        s.stats[slot * 256 + tid] = make_float2(top, sum);
+            for (int i = 0; i < 4; ++i) to[(d * 4 + i) * kThreads + tid] = f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
+        s.stats[slot * kThreads + tid] = make_float2(top, sum);
     }
 
     __device__ __forceinline__ void join(const Schedule &s, int64_t slot) {
         const int tid = (int)threadIdx.x;
-        const float2 st = s.stats[slot * 256 + tid];
+        const float2 st = s.stats[slot * kThreads + tid];
         const f32x4 *const from = (const f32x4 *)(s.sums + slot * (kWideRows * D));
         const float to = fmaxf(top, st.x), mine = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - to),
                     theirs = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.x - to);
@@ -761,12 +751,14 @@ struct Wide {
         for (int d = 0; d < kDims; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x4 x = from[(d * 4 + i) * 256 + tid];
+                const f32x4 x = from[(d * 4 + i) * kThreads + tid];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[d][i * 4 + e] = o[d][i * 4 + e] * mine + x[e] * theirs;
             }
     }
 };
+
+constexpr int64_t kWideLeast = 2;
 
 __device__ __forceinline__ WidePart wide_part(const PagedAttention &a, const Tile &t, int head) {
     const PagedRequest rq = paged_request(a.req, a.cache.page_shift, t.request);
@@ -784,13 +776,13 @@ template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kWideWaves * 64, 2) spd_paged_wide_kernel(const PagedAttention a, const Schedule s) {
     __shared__ __align__(16) half_t<T> s_kv[4 * kWideKeys * D];
     const int n_tiles = s.n_tiles[0];
-    if (n_tiles == 0) return;
-    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads, workers = workers_for(all, gridDim.x, 1);
     const int64_t w = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-    if (w >= workers) return;
-    int64_t at = share_begin(all, workers, w);
-    const int64_t end = share_begin(all, workers, w + 1);
-    Place place = find_place(s, n_tiles, per_head, at);
+    const int64_t per_head = n_tiles ? s.first[n_tiles] : 0, all = per_head * a.cache.kv_heads, workers = workers_for(all, gridDim.x, kWideLeast);
+    int64_t at = w < workers ? share_begin(all, workers, w) : all;
+    const int64_t end = w < workers ? share_begin(all, workers, w + 1) : all;
+    Joined joined{};
+    Place place{};
+    if (at < end) place = find_place(s, n_tiles, per_head, at);
     while (at < end) {
         const Tile t = s.tiles[place.tile];
         WidePart p = wide_part(a, t, place.head);
@@ -800,31 +792,30 @@ __global__ void __launch_bounds__(kWideWaves * 64, 2) spd_paged_wide_kernel(cons
         n.walk(a, p, s_kv);
         if (p.unit0 == 0 && p.unit1 == t.units) n.write(a, p);
         else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
+        if (p.unit0 == 0 && p.unit1 < t.units)
+            joined = Joined{(int)(worker_of(all, workers, place.segment_begin + t.units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, 0};
         at = place.segment_begin + p.unit1;
         if (p.unit1 == t.units) {
             place.segment_begin = at;
             if (++place.tile == n_tiles) { place.tile = 0; ++place.head; }
         }
     }
+    if (threadIdx.x == 0) s.joined[w] = joined;
 }
 
+// A workgroup to a worker, as for few rows.
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kWideWaves * 64) spd_paged_wide_join_kernel(const PagedAttention a, const Schedule s, const int most_workers) {
-    const int n_tiles = s.n_tiles[0];
-    if (n_tiles == 0) return;
-    const int64_t per_head = s.first[n_tiles], all = per_head * a.cache.kv_heads, workers = workers_for(all, most_workers, 1);
-    const int64_t w = (int64_t)blockIdx.x + 1;
-    if (w >= workers) return;
-    const int64_t at = share_begin(all, workers, w);
-    const Place place = find_place(s, n_tiles, per_head, at);
-    if (at == place.segment_begin || share_begin(all, workers, w - 1) > place.segment_begin) return;
-    const Tile t = s.tiles[place.tile];
-    const int64_t end = place.segment_begin + t.units;
+__global__ void __launch_bounds__(kWideWaves * 64) spd_paged_wide_join_kernel(const PagedAttention a, const Schedule s) {
+    const Joined j = s.joined[blockIdx.x];
+    if (j.parts == 0) return;
+    const int64_t w = blockIdx.x;
     Wide<T, D> n;
     n.clear();
-    n.join(s, 2 * (w - 1) + 1);
-    for (int64_t other = w; other < workers && share_begin(all, workers, other) < end; ++other) n.join(s, 2 * other);
-    n.write(a, wide_part(a, t, place.head));
+    n.join(s, 2 * w + 1);
+    for (int i = 1; i < j.parts; ++i) n.join(s, 2 * (w + i));
+    WidePart p{};
+    p.first_token = j.first_token; p.row0 = j.row0; p.rows = j.rows; p.head = j.head;
+    n.write(a, p);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -856,8 +847,8 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
     c.rows = c.wide ? kWideRows : kNarrowRows;
     c.keys = c.wide ? kWideKeys : kNarrowKeys;
     c.threads = c.wide ? kWideWaves * 64 : 64;
-    const int groups = std::max(n_cus / 8, 1) * 8 * 2;      // two to a compute unit, as many to every XCD
-    c.workers = c.wide ? groups : groups * kNarrowWaves;
+    const int groups = std::max(n_cus / 8, 1) * 8;          // as many to every XCD
+    c.workers = c.wide ? groups : groups * 2 * kNarrowWaves;
     c.tiles = rows / c.rows + a.req.n_requests;
     return c;
 }
@@ -870,6 +861,7 @@ size_t lay_out(const PagedAttention &a, const Cut &c, unsigned char *base, Sched
     if (a.selected) {
         slots = c.splits > 1 ? (size_t)a.req.n_tokens * (size_t)a.cache.kv_heads * (size_t)c.head_tiles * (size_t)c.splits : 0;
     } else {
+        s->joined = (Joined *)take((size_t)c.workers * sizeof(Joined));
         s->n_tiles = (int32_t *)take(4);
         s->first = (int64_t *)take((size_t)(c.tiles + 1) * 8);
         s->most_tiles = c.tiles;
@@ -896,10 +888,10 @@ hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Sc
     if (c.wide) {
         hipLaunchKernelGGL(spd_paged_schedule_kernel, dim3(1), dim3(kScheduleThreads), 0, st, a.req, a.cache.page_shift, a.q.group, c.rows, c.keys, s);
         hipLaunchKernelGGL((spd_paged_wide_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s);
-        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s, c.workers);
+        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s);
     } else {
         hipLaunchKernelGGL((spd_paged_narrow_kernel<T, D>), dim3((unsigned)(c.workers / kNarrowWaves)), dim3(kNarrowWaves * 64), 0, st, a, s);
-        hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kNarrowWaves * 64), 0, st, a, s, c.workers);
+        hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kNarrowWaves * 64), 0, st, a, s);
     }
     return hipGetLastError();
 }

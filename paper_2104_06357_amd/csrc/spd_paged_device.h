@@ -26,15 +26,34 @@ __device__ __forceinline__ PagedRequest paged_request(const PagedRequests &q, in
     return p;
 }
 
-// The request of a token: the last one that begins at or before it (-1: none).
-__device__ __forceinline__ int paged_request_of(const PagedRequests &q, int token) {
-    int lo = 0, hi = q.n_requests;                       // query_start[lo] <= token < query_start[hi], where there are such
-    if (q.n_requests == 0 || q.query_start[0] > token || q.query_start[hi] <= token) return -1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (q.query_start[mid] <= token) lo = mid; else hi = mid;
+// The request of a token (-1: none), which is the same for all lanes of the wavefront that look for it together: 64 requests are
+// looked at a time, and where there are no more the request's own numbers come along, one round trip to memory in all.
+__device__ __forceinline__ int paged_request_of(const PagedRequests &q, int page_shift, int token, PagedRequest &rq) {
+    const int lane = (int)threadIdx.x & 63, n = q.n_requests;
+    int r = -1;
+    if (n <= 64) {
+        const int at = min(lane, n - 1);
+        const PagedRequest mine = paged_request(q, page_shift, at);
+        const uint64_t has = __ballot(lane < n && token >= mine.first && token - mine.first < mine.count);
+        if (has == 0) return -1;
+        r = (int)__builtin_ctzll(has);
+        rq.first = __builtin_amdgcn_readlane(mine.first, r);
+        rq.count = __builtin_amdgcn_readlane(mine.count, r);
+        rq.kv = __builtin_amdgcn_readlane(mine.kv, r);
+        return r;
     }
-    return lo;
+    int lo = 0, hi = n;                                  // query_start[lo] <= token < query_start[hi], where there are such
+    if (q.query_start[0] > token || q.query_start[n] <= token) return -1;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+        const uint64_t under = __ballot(i < hi && q.query_start[i] <= token);
+        if (under == 0) return -1;                       // (numbers that descend)
+        lo = __builtin_amdgcn_readfirstlane(lo + (63 - (int)__builtin_clzll(under)) * step);
+        hi = min(hi, lo + step);
+    }
+    r = lo;
+    rq = paged_request(q, page_shift, r);
+    return token >= rq.first && token - rq.first < rq.count ? r : -1;
 }
 
 // ---- matrix products of 16-bit values and their operands -------------------------------------------
@@ -52,12 +71,28 @@ __device__ __forceinline__ f32x16 mfma32(half8_t<SPD_F16> a, half8_t<SPD_F16> b,
 __device__ __forceinline__ f32x4 mfma16(half8_t<SPD_BF16> a, half8_t<SPD_BF16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma16(half8_t<SPD_F16> a, half8_t<SPD_F16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+// LDS by its bytes: what is read together lies at one lane's offset, its low bits exclusive-or'ed with a constant, plus a constant.
+typedef __attribute__((address_space(3))) char *LdsBytes;
+__device__ __forceinline__ LdsBytes lds_bytes(void *p) { return (LdsBytes)(__attribute__((address_space(3))) void *)p; }
+template <spd_dtype T>
+__device__ __forceinline__ half8_t<T> read_row(LdsBytes p) { return *(const __attribute__((address_space(3))) half8_t<T> *)p; }
+template <spd_dtype T>
+__device__ __forceinline__ void write_row(LdsBytes p, half8_t<T> v) { *(__attribute__((address_space(3))) half8_t<T> *)p = v; }
 // Of every 16 lanes: lane s names 4 values, the columns 4 (s % 4) .. + 3 of row s / 4, and lane i gets column i of the four rows.
 template <spd_dtype T>
-__device__ __forceinline__ half4_t<T> read_transposed(const half_t<T> *lds) {
-    typedef __attribute__((address_space(3))) i16x4 *Lds;
-    return __builtin_bit_cast(half4_t<T>, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(uintptr_t)(__attribute__((address_space(3))) void *)lds));
+__device__ __forceinline__ half4_t<T> read_transposed(LdsBytes p) {
+    return __builtin_bit_cast(half4_t<T>, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)p));
 }
+// Two of those, `apart` bytes from each other, as the operand of a product.
+template <spd_dtype T>
+__device__ __forceinline__ half8_t<T> read_transposed(LdsBytes p, int apart) {
+    return __builtin_shufflevector(read_transposed<T>(p), read_transposed<T>(p + apart), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Where 16-byte chunk c of row r lies in a tile of K, read a chunk of many rows at a time, and of V, read transposed, 4 rows by 64
+// bytes: such rows in different banks.
+template <int D> __device__ __forceinline__ int k_at(int r, int c) { return r * D * 2 + (D == 128 ? (c ^ (r & 15)) : (c ^ ((r >> 1) & 7))) * 16; }
+template <int D> __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + (D == 128 ? (c ^ ((r & 3) << 2)) : (c ^ (((r >> 1) & 1) << 2))) * 16; }
 
 template <spd_dtype T>
 __device__ __forceinline__ half8_t<T> rounded(const float *x) {

@@ -23,63 +23,69 @@ constexpr uint32_t kForced = 0xffffffffu, kAbsent = 2;
 // A wavefront chooses the `k` greatest of `n` keys, equal ones by the lower number, and hands each to `take(rank, number)`, rank
 // ascending with the number.  Lane l holds the numbers l * each .. + each - 1, each <= kSelectEach.  The k-th key is found bit by bit: the keys at
 // or above a candidate are counted with a ballot to a register, and the search ends as soon as a candidate leaves k.
-template <typename Key, typename Take>
-__device__ __forceinline__ void choose(int n, int k, int each, Key key, Take take) {
+template <int kEach, typename Key, typename Take>
+__device__ __forceinline__ void choose_of(int n, int k, int each, Key key, Take take) {
     const int lane = (int)threadIdx.x & 63, first = lane * each;
-    uint32_t mine[kSelectEach];
+    uint32_t mine[kEach];
 #pragma unroll
-    for (int j = 0; j < kSelectEach; ++j) {
+    for (int j = 0; j < kEach; ++j) {
         mine[j] = 0;
         if (j < each && first + j < n) mine[j] = key(first + j);
     }
     uint32_t floor = 0;
     bool exact = false;                                           // as many as k lie at or above `floor`
+#pragma unroll 1
     for (int bit = 31; bit >= 0 && !exact; --bit) {
         const uint32_t to = floor | 1u << bit;
         int count = 0;
 #pragma unroll
-        for (int j = 0; j < kSelectEach; ++j) if (j < each) count += __popcll(__ballot(mine[j] >= to));
+        for (int j = 0; j < kEach; ++j) count += __popcll(__ballot(mine[j] >= to));
         if (count >= k) floor = to;
         exact = count == k;
     }
-    // those above the floor, and of those at it as many as are left, lower numbers first
-    int above = 0, at = 0;
+    // those above the floor, and of those at it as many as are left, lower numbers first: a bit to each of the lane's
+    uint64_t above = 0, at = 0;
 #pragma unroll
-    for (int j = 0; j < kSelectEach; ++j) if (j < each) { above += mine[j] > floor; at += mine[j] == floor && floor > 0; }
-    int both = above | at << 16, sum = both;
+    for (int j = 0; j < kEach; ++j) {
+        above |= (uint64_t)(mine[j] > floor) << j;
+        at |= (uint64_t)(mine[j] == floor && floor > 0) << j;
+    }
+    const int both = __popcll(above) | __popcll(at) << 16;
+    int sum = both;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) { const int up = __shfl_up(sum, d); if (lane >= d) sum += up; }
-    const int all = __shfl(sum, 63), left = k - (all & 0xffff);
-    int before_above = (sum - both) & 0xffff, before_at = (sum - both) >> 16;
-#pragma unroll
-    for (int j = 0; j < kSelectEach; ++j) {
-        if (j < each) {
-            const bool is_at = mine[j] == floor && floor > 0;
-            if (mine[j] > floor || (is_at && before_at < left)) take(before_above + min(before_at, left), first + j);
-            before_above += mine[j] > floor;
-            before_at += is_at;
-        }
-    }
+    const int left = k - (__shfl(sum, 63) & 0xffff), before = sum - both;
+    int rank = (before & 0xffff) + min(before >> 16, left), more = max(0, left - (before >> 16));
+    for (uint64_t rest = at; rest != 0; rest &= rest - 1, --more) if (more > 0) above |= rest & -rest;
+    for (; above != 0; above &= above - 1) take(rank++, first + (int)__builtin_ctzll(above));
+}
+
+// (a register that holds no key costs as much as one that does)
+template <typename Key, typename Take>
+__device__ __forceinline__ void choose(int n, int k, int each, Key key, Take take) {
+    if (each <= 5) choose_of<5>(n, k, each, key, take);
+    else if (each <= 9) choose_of<9>(n, k, each, key, take);
+    else if (each <= 17) choose_of<17>(n, k, each, key, take);
+    else choose_of<kSelectEach>(n, k, each, key, take);
 }
 
 struct Candidate { uint32_t key; int32_t page; };
 
 // A tile of tokens: workgroups `b` < blocks have the tokens from 16 b to the end of the block or of the request that 16 b is in, the others
 // the first tokens of request b - blocks, where it begins inside a block.
-struct TokenTile { int request, first, count; };
-__device__ __forceinline__ TokenTile token_tile(const PagedRequests &req, int b, int blocks) {
-    TokenTile t{-1, 0, 0};
+struct TokenTile { int request, first, count; PagedRequest rq; };
+__device__ __forceinline__ TokenTile token_tile(const PagedRequests &req, int page_shift, int b, int blocks) {
+    TokenTile t{-1, 0, 0, {}};
     if (b < blocks) {
         t.first = b * kSelectTokens;
-        t.request = paged_request_of(req, t.first);
+        t.request = paged_request_of(req, page_shift, t.first, t.rq);
     } else {
         t.request = b - blocks;
-        t.first = max(req.query_start[t.request], 0);
+        t.rq = paged_request(req, page_shift, t.request);
+        t.first = t.rq.first;
         if (t.first % kSelectTokens == 0) t.request = -1;
     }
-    if (t.request < 0) return t;
-    const int end = min(min(max(req.query_start[t.request + 1], 0), req.n_tokens), (t.first / kSelectTokens + 1) * kSelectTokens);
-    t.count = max(0, end - t.first);
+    if (t.request >= 0) t.count = max(0, min(t.rq.first + t.rq.count, (t.first / kSelectTokens + 1) * kSelectTokens) - t.first);
     return t;
 }
 
@@ -95,18 +101,46 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
     extern __shared__ __align__(16) uint32_t s_key[];             // [16][room]
     __shared__ __align__(16) int8_t s_code[kSelectTokens][2 * D];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kvh = (int)blockIdx.y, group = a.q.group, chunk = (int)blockIdx.z;
-    const TokenTile tile = token_tile(a.req, (int)blockIdx.x, blocks);
+    const TokenTile tile = token_tile(a.req, a.cache.page_shift, (int)blockIdx.x, blocks);
     if (tile.count == 0) return;
-    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, tile.request);
+    const PagedRequest &rq = tile.rq;
     const int position0 = rq.kv - rq.count + tile.first - rq.first, shift = a.cache.page_shift;
     const int page0 = chunk * kSelectPages, most = position0 + tile.count - 1 < 0 ? 0 : ((position0 + tile.count - 1) >> shift) + 1;     // pages that the last token sees
     if (page0 > 0 && page0 >= most) return;
     const int pages = min(most - page0, kSelectPages);            // of this workgroup
     if (most > a.n_select) {
+        const int low = lane & 15, quad = lane >> 4;
+        const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride + page0;
+        i32x4 c[kSteps];
+        float scale;
+        auto fetch = [&](int p0) {
+            const int32_t number = p0 + low < pages ? table[p0 + low] : -1;
+            const bool there = number >= 0 && number < a.cache.n_pages;
+            const int64_t at = (int64_t)(there ? number : 0) * a.cache.kv_heads + kvh;
+            scale = -__builtin_inff();                            // (marks a page that is not there)
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) c[s] = i32x4{0, 0, 0, 0};
+            if (there) {
+                const int8_t *const from = a.cache.codes + at * 2 * D + quad * 16;
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) c[s] = *(const i32x4 *)(from + s * 64);
+                scale = a.cache.code_scale[at];
+            }
+        };
+        if (wave * 16 < pages) fetch(wave * 16);                  // (on its way while the queries are)
         if (wave < tile.count) {
             const H *const q = (const H *)a.q.ptr + (int64_t)(tile.first + wave) * a.q.token_stride + (int64_t)kvh * group * a.q.head_stride + lane * E;
-            float big = 0.0f;
-            for (int g = 0; g < group; ++g)
+            constexpr int kHeld = 8;                              // heads that stay in registers between the two passes
+            float held[kHeld][E], big = 0.0f;
+#pragma unroll
+            for (int g = 0; g < kHeld; ++g)
+#pragma unroll
+                for (int e = 0; e < E; ++e) held[g][e] = g < group ? (float)q[g * a.q.head_stride + e] : 0.0f;
+#pragma unroll
+            for (int g = 0; g < kHeld; ++g)
+#pragma unroll
+                for (int e = 0; e < E; ++e) big = fmaxf(big, fabsf(held[g][e]));
+            for (int g = kHeld; g < group; ++g)
 #pragma unroll
                 for (int e = 0; e < E; ++e) big = fmaxf(big, fabsf((float)q[g * a.q.head_stride + e]));
 #pragma unroll
@@ -115,12 +149,18 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
             int up[E], down[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) up[e] = down[e] = 0;
-            for (int g = 0; g < group; ++g)
+            auto add = [&](int e, float x) {
+                const int code = step > 0.0f ? (int)rintf(x / step) : 0;
+                up[e] += max(code, 0); down[e] += max(-code, 0);
+            };
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int c = step > 0.0f ? (int)rintf((float)q[g * a.q.head_stride + e] / step) : 0;
-                    up[e] += max(c, 0); down[e] += max(-c, 0);
-                }
+            for (int g = 0; g < kHeld; ++g)
+                if (g < group)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) add(e, held[g][e]);
+            for (int g = kHeld; g < group; ++g)
+#pragma unroll
+                for (int e = 0; e < E; ++e) add(e, (float)q[g * a.q.head_stride + e]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 s_code[wave][lane * E + e] = (int8_t)-(int)rintf((float)down[e] * share);
@@ -131,33 +171,20 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
             for (int e = 0; e < 2 * E; ++e) s_code[wave][lane * 2 * E + e] = 0;
         }
         __syncthreads();
-        const int low = lane & 15, quad = lane >> 4;
         i32x4 q[kSteps];
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = *(const i32x4 *)&s_code[low][s * 64 + quad * 16];
-        const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride + page0;
         const int own = low < tile.count && position0 + low >= 0 ? (position0 + low) >> shift : -1;    // of token `low`
         for (int p0 = wave * 16; p0 < pages; p0 += kSelectTokens * 16) {
-            const int32_t number = p0 + low < pages ? table[p0 + low] : -1;
-            const bool there = number >= 0 && number < a.cache.n_pages;
-            const int64_t at = (int64_t)(there ? number : 0) * a.cache.kv_heads + kvh;
-            i32x4 c[kSteps];
-            float scale = -__builtin_inff();                      // (marks a page that is not there)
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) c[s] = i32x4{0, 0, 0, 0};
-            if (there) {
-                const int8_t *const from = a.cache.codes + at * 2 * D + quad * 16;
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s) c[s] = *(const i32x4 *)(from + s * 64);
-                scale = a.cache.code_scale[at];
-            }
             i32x4 x = {0, 0, 0, 0};
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_i32_16x16x64_i8(c[s], q[s], x, 0, 0, 0);
+            const float scale_now = scale;
+            if (p0 + kSelectTokens * 16 < pages) fetch(p0 + kSelectTokens * 16);
             uint32_t key[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float of_page = __shfl(scale, quad * 4 + i);
+                const float of_page = __shfl(scale_now, quad * 4 + i);
                 const int p = page0 + p0 + quad * 4 + i;
                 key[i] = of_page == -__builtin_inff() ? kAbsent : key_of((float)x[i] * of_page);
                 if (p == 0 || p == own) key[i] = kForced;
@@ -192,9 +219,9 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
 __global__ void __launch_bounds__(64) spd_paged_select_join_kernel(const PagedAttention a, int32_t *const selected, Candidate *const candidates,
                                                                     const int chunks) {
     const int lane = (int)threadIdx.x & 63, t = (int)blockIdx.x, kvh = (int)blockIdx.y, k = a.n_select;
-    const int r = paged_request_of(a.req, t);
+    PagedRequest rq;
+    const int r = paged_request_of(a.req, a.cache.page_shift, t, rq);
     if (r < 0) return;
-    const PagedRequest rq = paged_request(a.req, a.cache.page_shift, r);
     const int position = rq.kv - rq.count + (t - rq.first), sees = position < 0 ? 0 : (position >> a.cache.page_shift) + 1;
     if (sees <= kSelectPages) return;
     Candidate *const from = candidates + ((int64_t)t * a.cache.kv_heads + kvh) * chunks * k;
