@@ -2076,7 +2076,7 @@ spd_status spd_paged_workspace_bytes(const spd_handle *h, const spd_paged_cache 
     PagedAttention a = paged_attention_args(*c, *b, n_heads);
     a.n_select = n_select;
     a.selected = n_select > 0 ? reinterpret_cast<const int32_t *>(bytes) : nullptr;      // (only looked at for being there)
-    *bytes = align256(paged_attention_scratch(a, h->opt.n_cus)) + (n_select > 0 ? align256(paged_select_scratch(a)) : 0);
+    *bytes = std::max<size_t>(256, align256(paged_attention_scratch(a, h->opt.n_cus)) + (n_select > 0 ? align256(paged_select_scratch(a)) : 0));
     return SPD_OK;
 }
 

@@ -17,7 +17,7 @@ constexpr float kSlack = 8.0f;          // a row's maximum is moved (and its sum
 // another kernel joins them.
 
 struct Tile { int32_t request, row0, units, pad; };
-struct Joined { int32_t parts, request, first_token, position0, row0, rows, head, pad; };        // parts: 0 if there is no such segment
+struct Joined { int32_t parts, request, first_token, position0, row0, rows, head, worker; };     // parts: 0 if there is no such segment
 struct Schedule {
     int64_t *first;                     // [tiles + 1]: units of the tiles before
     Tile *tiles;
@@ -279,8 +279,7 @@ struct Narrow {
             float big = w[0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
-            big = fmaxf(big, __shfl_xor(big, 16));
-            big = fmaxf(big, __shfl_xor(big, 32)) * a.q.scale;
+            big = greatest_of_4(big) * a.q.scale;
             if (__any(big > top + kSlack)) {
                 const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
                 top = to;
@@ -295,11 +294,11 @@ struct Narrow {
 #pragma unroll
             for (int d = 0; d < kDims; ++d) o[d] = mfma16(read_transposed<T>(s_v + (v_lane ^ (d << 5)), 32 * D), pw, o[d]);
         }
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
+        sum = sum_of_4(sum);
     }
 
-    __device__ __forceinline__ void write(const PagedAttention &a, const NarrowPart &p) const {
+    // Of the sums' 16-place pieces those of member `me` of a team of `team` wavefronts.
+    __device__ __forceinline__ void write(const PagedAttention &a, const NarrowPart &p, int team, int me) const {
         const int lane = (int)threadIdx.x & 63, row = lane & 15, quad = lane >> 4;
         if (row >= p.rows) return;
         const int f = p.row0 + row, token = SELECTED ? 0 : f / a.q.group, g = SELECTED ? f : f - token * a.q.group;
@@ -307,20 +306,50 @@ struct Narrow {
         const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
+            if ((d & (team - 1)) != me) continue;
             half4_t<T> r;
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[i] = (H)(o[d][i] * by);
             *(half4_t<T> *)((H *)a.out.out + at * D + d * 16 + quad * 4) = r;
         }
-        if (quad == 0 && a.out.lse) a.out.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
+        if (me == 0 && quad == 0 && a.out.lse) a.out.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
     }
 
-    __device__ __forceinline__ void leave(const Schedule &s, int64_t slot) const {
+    __device__ __forceinline__ void leave(const Schedule &s, int64_t slot, int team, int me) const {
         const int lane = (int)threadIdx.x & 63;
         f32x4 *const to = (f32x4 *)(s.sums + slot * (kNarrowRows * D));
 #pragma unroll
-        for (int d = 0; d < kDims; ++d) to[d * 64 + lane] = o[d];
-        s.stats[slot * 64 + lane] = make_float2(top, sum);
+        for (int d = 0; d < kDims; ++d) if ((d & (team - 1)) == me) to[d * 64 + lane] = o[d];
+        if (me == 0) s.stats[slot * 64 + lane] = make_float2(top, sum);
+    }
+
+    // The wavefronts of a workgroup, each with its sums, join them: each gets its own pieces of the whole.  regions: of each wavefront, where its keys
+    // were (they are done with), stats: of each.  All of the workgroup come here.
+    template <int kTeam, typename Region>
+    __device__ __forceinline__ void join_team(Region regions, float2 (*stats)[64], int me) {
+        const int lane = (int)threadIdx.x & 63;
+        f32x4 (*const mine)[64] = (f32x4 (*)[64])regions(me);
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) mine[d][lane] = o[d];
+        stats[me][lane] = make_float2(top, sum);
+        __syncthreads();
+        float2 st[kTeam];
+        top = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < kTeam; ++i) { st[i] = stats[i][lane]; top = fmaxf(top, st[i].x); }
+        const float from = top == -__builtin_inff() ? 0.0f : top;
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kTeam; ++i) { st[i].x = __builtin_amdgcn_exp2f(st[i].x - from); sum += st[i].x * st[i].y; }
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            if ((d & (kTeam - 1)) != me) continue;
+            f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kTeam; ++i) x += ((const f32x4 (*)[64])regions(i))[d][lane] * st[i].x;
+            o[d] = x;
+        }
+        __syncthreads();
     }
 
     // Takes in another part's sums.
@@ -375,31 +404,34 @@ __device__ __forceinline__ NarrowPart narrow_part(const PagedAttention &a, const
     return p;
 }
 
-// Where the workers' shares begin and end, for few requests: every wavefront counts the tiles and units itself, a request to a lane, instead
-// of reading them from another kernel's arrays.
+// Where the workers' shares begin and end: every wavefront counts the tiles and units itself, a request to a lane, instead
+// of waiting for another kernel to do it.  (The host takes care that a key head's units are fewer than 2^31.)
 struct Counted {
     const PagedAttention *a;
-    int64_t per_head;                   // units
-    int tiles, units;                   // of the lane's request, of the last 64 that were counted
-    int64_t upto;                       // units of the requests up to it
+    int32_t per_head, tiles;            // units and tiles
+    PagedRequest rq;                    // the lane's request, of the last 64 that were counted
+    int32_t upto;                       // units of the requests up to it
 
-    __device__ __forceinline__ void count(int base, int64_t before) {
+    __device__ __forceinline__ int count(int base, int before) {
         const int r = base + ((int)threadIdx.x & 63);
-        tiles = 0;
-        int64_t u = 0;
+        int many = 0, u = 0;
         if (r < a->req.n_requests) {
-            const PagedRequest rq = paged_request(a->req, a->cache.page_shift, r);
-            tiles = (rq.count * a->q.group + kNarrowRows - 1) / kNarrowRows;
-            for (int i = 0; i < tiles; ++i) u += tile_units(rq, a->q.group, kNarrowRows, kNarrowKeys, i);
+            rq = paged_request(a->req, a->cache.page_shift, r);
+            many = (rq.count * a->q.group + kNarrowRows - 1) / kNarrowRows;
+            for (int i = 0; i < many; ++i) u += tile_units(rq, a->q.group, kNarrowRows, kNarrowKeys, i);
         }
-        int64_t sum = u;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) { const int64_t up = __shfl_up(sum, d); if (((int)threadIdx.x & 63) >= d) sum += up; }
-        units = (int)u;
-        upto = before + sum;
+        upto = before + sum_upto(u);
+        return many;
     }
-    __device__ __forceinline__ explicit Counted(const PagedAttention &args) : a(&args), per_head(0), tiles(0), units(0), upto(0) {
-        for (int base = 0; base < a->req.n_requests; base += 64) { count(base, per_head); per_head = uniform(__shfl(upto, 63)); }
+    __device__ __forceinline__ explicit Counted(const PagedAttention &args) : a(&args), per_head(0), tiles(0), rq{0, 0, 0}, upto(0) {
+        for (int base = 0; base < a->req.n_requests; base += 64) {
+            tiles += from_lane(sum_upto(count(base, per_head)), 63);
+            per_head = from_lane(upto, 63);
+        }
+    }
+    __device__ __forceinline__ PagedRequest request(int r) const {
+        if (a->req.n_requests > 64) return paged_request(a->req, a->cache.page_shift, r);
+        return PagedRequest{from_lane(rq.first, r), from_lane(rq.count, r), from_lane(rq.kv, r)};
     }
 };
 
@@ -408,144 +440,159 @@ struct Cursor {
     PagedRequest rq;
     int request, tile, tiles, head;
     int64_t begin;                      // the segment's first unit
-    __device__ __forceinline__ void enter(const PagedAttention &a, int r) {
+    __device__ __forceinline__ void enter(const Counted &c, int r) {
         request = uniform(r);
-        rq = paged_request(a.req, a.cache.page_shift, request);
-        tiles = (rq.count * a.q.group + kNarrowRows - 1) / kNarrowRows;
+        rq = c.request(request);
+        tiles = (rq.count * c.a->q.group + kNarrowRows - 1) / kNarrowRows;
         tile = 0;
     }
-    __device__ __forceinline__ int units(const PagedAttention &a) const { return tile_units(rq, a.q.group, kNarrowRows, kNarrowKeys, tile); }
-    __device__ __forceinline__ void find(Counted &c, const PagedAttention &a, int64_t at) {
-        head = (int)(at / c.per_head);
-        const int64_t x = at - head * c.per_head;
-        int64_t before = 0;
-        for (int base = 0;; base += 64) {
-            if (a.req.n_requests > 64) c.count(base, before);
-            const int64_t to = uniform(__shfl(c.upto, 63));
-            if (x < to || base + 64 >= a.req.n_requests) {
-                const int lane = (int)__builtin_ctzll(__ballot(c.upto > x));
-                begin = head * c.per_head + (lane ? uniform(__shfl(c.upto, lane - 1)) : before);
-                enter(a, base + lane);
+    __device__ __forceinline__ int units(const Counted &c) const { return tile_units(rq, c.a->q.group, kNarrowRows, kNarrowKeys, tile); }
+    __device__ __forceinline__ void find(Counted &c, int64_t at) {
+        head = uniform((int)(at / c.per_head));
+        const int64_t start = (int64_t)head * c.per_head;
+        const int x = (int)(at - start);
+        for (int base = 0, before = 0;; base += 64) {
+            if (c.a->req.n_requests > 64) c.count(base, before);
+            const int to = from_lane(c.upto, 63);
+            if (x < to || base + 64 >= c.a->req.n_requests) {
+                const int lane = uniform((int)__builtin_ctzll(__ballot(c.upto > x)));
+                begin = start + (lane ? from_lane(c.upto, lane - 1) : before);
+                enter(c, base + lane);
                 break;
             }
             before = to;
         }
-        for (int u = units(a); at >= begin + u; u = units(a)) { begin += u; ++tile; }
+        for (int u = units(c); at >= begin + u; u = units(c)) { begin += u; ++tile; }
     }
-    __device__ __forceinline__ void next(const PagedAttention &a, int units) {
+    __device__ __forceinline__ void next(const Counted &c, int units) {
         begin += units;
         if (++tile < tiles) return;
         int r = request;
-        do { if (++r == a.req.n_requests) { r = 0; ++head; } enter(a, r); } while (tiles == 0);
+        do { if (++r == c.a->req.n_requests) { r = 0; ++head; } enter(c, r); } while (tiles == 0);
     }
 };
 
-// What a worker does at the least: parts of one unit would cost more to join than they save.
-constexpr int64_t kNarrowLeast = 2;
+// Workers are whole workgroups where segments are long (a part's sums are then joined in LDS, a quarter as many go through scratch), and
+// wavefronts of their own where they are short (no wavefront waits for others).
+constexpr int kLongSegment = 16, kNarrowLeast = 2;      // units; of a wavefront at the least, since each more part is more to join
 
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(const PagedAttention a, const Schedule s) {
     __shared__ __align__(16) half_t<T> s_kv[kNarrowWaves][2 * kNarrowKeys * D];
+    __shared__ float2 s_stats[kNarrowWaves][64];
     const int wave = uniform((int)threadIdx.x >> 6);
     Counted counted(a);
-    const int64_t all = counted.per_head * a.cache.kv_heads;
-    const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves, kNarrowLeast);
+    const int team = counted.per_head / kLongSegment >= counted.tiles ? kNarrowWaves : 1, me = team == 1 ? 0 : wave;
+    const int64_t all = (int64_t)counted.per_head * a.cache.kv_heads;
+    const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves / team, kNarrowLeast * team);
     // neighbours in the units' order share an XCD and its L2 (workgroups go to the XCDs in turn)
-    const int64_t group = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = group * kNarrowWaves + wave;
+    const int64_t group = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = team == 1 ? group * kNarrowWaves + wave : group;
     int64_t at = w < workers ? share_begin(all, workers, w) : all;
     const int64_t end = w < workers ? share_begin(all, workers, w + 1) : all;
     Joined joined{};
     Cursor c;
-    if (at < end) c.find(counted, a, at);
+    if (at < end) c.find(counted, at);
     while (at < end) {
-        const int units = c.units(a);
+        const int units = c.units(counted), unit0 = uniform((int)(at - c.begin)), unit1 = uniform((int)min((int64_t)units, end - c.begin));
         NarrowPart p = narrow_part(a, c.rq, c.request, c.tile * kNarrowRows, c.head);
-        p.unit0 = uniform((int)(at - c.begin));
-        p.unit1 = uniform((int)min((int64_t)units, end - c.begin));
+        p.unit0 = unit0; p.unit1 = unit1;
+        if (team > 1) {
+            p.unit0 = unit0 + (int)((uint32_t)(unit1 - unit0) * (uint32_t)me / kNarrowWaves);
+            p.unit1 = unit0 + (int)((uint32_t)(unit1 - unit0) * (uint32_t)(me + 1) / kNarrowWaves);
+        }
         Narrow<T, D, false> n;
-        n.walk(a, p, s_kv[wave]);
-        if (p.unit0 == 0 && p.unit1 == units) n.write(a, p);
-        else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
-        if (p.unit0 == 0 && p.unit1 < units)
-            joined = Joined{(int)(worker_of(all, workers, c.begin + units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, 0};
-        at = c.begin + p.unit1;
-        if (at < end) c.next(a, units);
+        if (p.unit0 < p.unit1) n.walk(a, p, s_kv[wave]); else n.clear();
+        if (team > 1) n.template join_team<kNarrowWaves>([&](int i) { return s_kv[i]; }, s_stats, me);
+        if (unit0 == 0 && unit1 == units) n.write(a, p, team, me);
+        else n.leave(s, 2 * w + (unit0 == 0 ? 1 : 0), team, me);
+        if (unit0 == 0 && unit1 < units)
+            joined = Joined{(int)(worker_of(all, workers, c.begin + units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, (int)w};
+        at = c.begin + unit1;
+        if (at < end) c.next(counted, units);
     }
-    if (((int)threadIdx.x & 63) == 0) s.joined[w] = joined;
+    if (me > 0) joined.parts = 0;
+    if (((int)threadIdx.x & 63) == 0) s.joined[group * kNarrowWaves + wave] = joined;
 }
 
-// A workgroup to a worker: the segment that it began and others went on with, if there is one.  The wavefronts take its parts in turn, then
-// each other's.
+// A workgroup to a segment that a worker began and others went on with, if there is one.  The wavefronts take its parts in turn, then each
+// other's.
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kNarrowWaves * 64) spd_paged_narrow_join_kernel(const PagedAttention a, const Schedule s) {
-    __shared__ __align__(16) f32x4 s_o[kNarrowWaves - 1][D / 16][64];
-    __shared__ float2 s_stats[kNarrowWaves - 1][64];
-    const int wave = uniform((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
+    __shared__ __align__(16) f32x4 s_o[kNarrowWaves][D / 16][64];
+    __shared__ float2 s_stats[kNarrowWaves][64];
+    const int wave = uniform((int)threadIdx.x >> 6);
     const Joined j = s.joined[blockIdx.x];
     if (j.parts == 0) return;
-    const int64_t w = blockIdx.x;
+    const int64_t w = j.worker;
     Narrow<T, D, false> n;
     n.clear();
     n.join_all(s, j.parts, wave, kNarrowWaves, [&](int i) { return i == 0 ? 2 * w + 1 : 2 * (w + i); });
-    if (wave > 0) {
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) s_o[wave - 1][d][lane] = n.o[d];
-        s_stats[wave - 1][lane] = make_float2(n.top, n.sum);
-    }
-    __syncthreads();
-    if (wave > 0) return;
-#pragma unroll
-    for (int i = 0; i < kNarrowWaves - 1; ++i) n.take(s_stats[i][lane], s_o[i], lane);
+    n.template join_team<kNarrowWaves>([&](int i) { return s_o[i]; }, s_stats, wave);
     NarrowPart p{};
     p.first_token = j.first_token; p.row0 = j.row0; p.rows = j.rows; p.head = j.head;
-    n.write(a, p);
+    n.write(a, p, kNarrowWaves, wave);
 }
 
-// Selected pages: a segment is a token, a key head and 16 of its query heads, cut into `splits` equal parts.
-template <spd_dtype T, int D, bool JOIN>
-__global__ void __launch_bounds__(JOIN ? 64 : kNarrowWaves * 64, JOIN ? 1 : 2)
-    spd_paged_selected_kernel(const PagedAttention a, const Schedule s, const int splits, const int head_tiles) {
-    __shared__ __align__(16) half_t<T> s_kv[JOIN ? 1 : kNarrowWaves][JOIN ? 8 : 2 * kNarrowKeys * D];
-    const int lane = (int)threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    // (a token's and its neighbours' segments share pages: neighbours share an XCD)
-    const int64_t blocks = (int64_t)gridDim.x, per = blocks / 8, rest = blocks % 8, xcd = blockIdx.x % 8;
-    const int64_t block = JOIN ? (int64_t)blockIdx.x : xcd * per + min(xcd, rest) + blockIdx.x / 8;
-    const int64_t w = JOIN ? block : block * kNarrowWaves + wave;
-    const int64_t segment = JOIN ? w : w / splits;
-    const int split = JOIN ? 0 : (int)(w % splits);
-    const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * head_tiles;
-    if (segment >= segments) return;
+// Selected pages: a segment is a token, a key head and 16 of its query heads.  With many of them each is a wavefront's; with few a
+// workgroup's, whose wavefronts share its units, and where even that leaves wavefronts with many units, several workgroups' (`splits`).
+constexpr int kSelectedTeam = 8;
+
+__device__ __forceinline__ bool selected_part(const PagedAttention &a, int64_t segment, int head_tiles, NarrowPart &p, int &units) {
+    const int lane = (int)threadIdx.x & 63;
+    if (segment >= (int64_t)a.req.n_tokens * a.cache.kv_heads * head_tiles) return false;
     const int tile = (int)(segment % head_tiles);
-    const int64_t rest_of = segment / head_tiles;
-    const int token = (int)(rest_of % a.req.n_tokens), head = (int)(rest_of / a.req.n_tokens);
+    const int64_t rest = segment / head_tiles;
+    const int token = uniform((int)(rest % a.req.n_tokens));
+    p.head = uniform((int)(rest / a.req.n_tokens));
+    // the list, whose last page is the token's own, on its way while the request is looked for
+    const int32_t *const list = a.selected + ((int64_t)token * a.cache.kv_heads + p.head) * a.n_select;
+    const int mine = lane < a.n_select ? list[lane] : -1;
     PagedRequest rq;
-    const int r = paged_request_of(a.req, a.cache.page_shift, uniform(token), rq);
-    if (r < 0) return;
-    NarrowPart p;
+    const int r = paged_request_of(a.req, a.cache.page_shift, token, rq);
+    if (r < 0) return false;
     p.request = uniform(r);
-    p.first_token = uniform(token); p.count = 1;
+    p.first_token = token; p.count = 1;
     p.position0 = uniform(rq.kv - rq.count + token - rq.first);
     p.row0 = tile * kNarrowRows;
     p.rows = min(kNarrowRows, a.q.group - p.row0);
-    p.head = uniform(head);
-    // pages in the list, the last of which is the token's own
-    const int32_t *const list = a.selected + ((int64_t)token * a.cache.kv_heads + head) * a.n_select;
-    const int many = __popcll(__ballot(lane < a.n_select && list[lane] >= 0));
-    const int shift = a.cache.page_shift;
+    const int many = __popcll(__ballot(mine >= 0)), shift = a.cache.page_shift;
     p.subs = many == 0 ? 0 : uniform(((many - 1) << (shift - 4)) + ((p.position0 & ((1 << shift) - 1)) >> 4) + 1);
-    const int units = max(1, (p.subs + 1) / 2);
+    units = max(1, (p.subs + 1) / 2);
+    return true;
+}
+
+template <spd_dtype T, int D, int TEAM>
+__global__ void __launch_bounds__((TEAM == 1 ? kNarrowWaves : TEAM) * 64, 2)
+    spd_paged_selected_kernel(const PagedAttention a, const Schedule s, const int splits, const int head_tiles) {
+    constexpr int kWaves = TEAM == 1 ? kNarrowWaves : TEAM;
+    __shared__ __align__(16) half_t<T> s_kv[kWaves][2 * kNarrowKeys * D];
+    __shared__ float2 s_stats[TEAM == 1 ? 1 : TEAM][64];
+    const int wave = uniform((int)threadIdx.x >> 6), me = TEAM == 1 ? 0 : wave;
+    // (a token's and its neighbours' segments share pages: neighbours share an XCD)
+    const int64_t blocks = (int64_t)gridDim.x, per = blocks / 8, rest = blocks % 8, xcd = blockIdx.x % 8;
+    const int64_t block = xcd * per + min(xcd, rest) + blockIdx.x / 8;
+    const int64_t w = TEAM == 1 ? block * kWaves + wave : block;
+    const int split = (int)(w % splits) * TEAM + me;
+    NarrowPart p;
+    int units;
+    if (!selected_part(a, w / splits, head_tiles, p, units)) return;
+    p.unit0 = uniform((int)share_begin(units, (int64_t)splits * TEAM, split));
+    p.unit1 = uniform((int)share_begin(units, (int64_t)splits * TEAM, split + 1));
     Narrow<T, D, true> n;
-    if (JOIN) {
-        n.clear();
-        n.join_all(s, min(units, splits), 0, 1, [&](int i) { return segment * splits + i; });
-        n.write(a, p);
-        return;
-    }
-    p.unit0 = uniform((int)share_begin(units, splits, split));
-    p.unit1 = uniform((int)share_begin(units, splits, split + 1));
-    if (p.unit0 == p.unit1) return;
-    n.walk(a, p, s_kv[JOIN ? 0 : wave]);
-    if (splits == 1) n.write(a, p); else n.leave(s, w);
+    if (p.unit0 < p.unit1) n.walk(a, p, s_kv[wave]); else n.clear();
+    if (TEAM > 1) n.template join_team<TEAM>([&](int i) { return s_kv[i]; }, s_stats, me);
+    if (splits == 1) n.write(a, p, TEAM, me); else n.leave(s, w, TEAM, me);
+}
+
+template <spd_dtype T, int D>
+__global__ void __launch_bounds__(64) spd_paged_selected_join_kernel(const PagedAttention a, const Schedule s, const int splits, const int head_tiles) {
+    NarrowPart p;
+    int units;
+    if (!selected_part(a, blockIdx.x, head_tiles, p, units)) return;
+    Narrow<T, D, true> n;
+    n.clear();
+    n.join_all(s, splits, 0, 1, [&](int i) { return (int64_t)blockIdx.x * splits + i; });
+    n.write(a, p, 1, 0);
 }
 
 // ---- many rows: a workgroup to 256 of them -------------------------------------------------------
@@ -661,7 +708,7 @@ struct Wide {
             float big = x[0][0];
 #pragma unroll
             for (int i = 1; i < 32; ++i) big = fmaxf(big, x[i >> 4][i & 15]);
-            big = fmaxf(big, __shfl_xor(big, 32)) * a.q.scale;
+            big = greatest_of_2(big) * a.q.scale;
             if (__any(big > top + kSlack)) {
                 const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
                 top = to;
@@ -708,7 +755,7 @@ struct Wide {
             ++u;
         }
         __syncthreads();                                // (the next segment's first unit goes where this one's last may be)
-        sum += __shfl_xor(sum, 32);
+        sum = sum_of_2(sum);
     }
 
     __device__ __forceinline__ void write(const PagedAttention &a, const WidePart &p) const {
@@ -825,7 +872,7 @@ size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 struct Cut {
     bool wide;
     int rows, keys, workers, threads;   // threads: of a worker
-    int splits, head_tiles;             // of selected segments
+    int splits, head_tiles, team;       // of selected segments
     int64_t tiles;                      // at most
 };
 
@@ -835,15 +882,17 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
     if (a.selected) {
         c.rows = kNarrowRows; c.keys = kNarrowKeys; c.threads = 64;
         c.head_tiles = (a.q.group + kNarrowRows - 1) / kNarrowRows;
-        const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles;
-        const int64_t units = std::max<int64_t>(1, ((int64_t)a.n_select << a.cache.page_shift) / kNarrowKeys);
-        const int64_t want = (int64_t)n_cus * 8;
-        c.splits = (int)std::max<int64_t>(1, std::min(units, want / std::max<int64_t>(segments, 1)));
+        const int64_t segments = std::max<int64_t>(1, (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles);
+        const int64_t units = ((int64_t)a.n_select << a.cache.page_shift) / kNarrowKeys;
+        c.team = segments >= (int64_t)n_cus * 8 ? 1 : kSelectedTeam;
+        // up to 8 units of a wavefront cost less than a second launch that joins (4 us)
+        c.splits = c.team == 1 ? 1 : (int)std::max<int64_t>(1, std::min(units / (kSelectedTeam * 8), n_cus / segments));
         c.workers = 0;
         return c;
     }
-    // (a wavefront of the narrow kernel counts 64 requests at a time)
-    c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256;
+    // A wavefront of the narrow kernel counts the units itself, 64 requests at a time and in 32 bits.
+    const int64_t most_units = (rows / kNarrowRows + a.req.n_requests) * ((((int64_t)a.req.max_pages << a.cache.page_shift) + kNarrowKeys - 1) / kNarrowKeys + 1);
+    c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256 || most_units >= (int64_t)1 << 31;
     c.rows = c.wide ? kWideRows : kNarrowRows;
     c.keys = c.wide ? kWideKeys : kNarrowKeys;
     c.threads = c.wide ? kWideWaves * 64 : 64;
@@ -878,11 +927,15 @@ size_t lay_out(const PagedAttention &a, const Cut &c, unsigned char *base, Sched
 template <spd_dtype T, int D>
 hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Schedule &s) {
     if (a.selected) {
-        const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles, waves = segments * c.splits;
-        hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, false>), dim3((unsigned)((waves + kNarrowWaves - 1) / kNarrowWaves)),
-                           dim3(kNarrowWaves * 64), 0, st, a, s, c.splits, c.head_tiles);
+        const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles;
+        if (c.team == 1)
+            hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, 1>), dim3((unsigned)((segments + kNarrowWaves - 1) / kNarrowWaves)),
+                               dim3(kNarrowWaves * 64), 0, st, a, s, 1, c.head_tiles);
+        else
+            hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, kSelectedTeam>), dim3((unsigned)(segments * c.splits)), dim3(kSelectedTeam * 64), 0, st,
+                               a, s, c.splits, c.head_tiles);
         if (c.splits > 1)
-            hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, true>), dim3((unsigned)segments), dim3(64), 0, st, a, s, c.splits, c.head_tiles);
+            hipLaunchKernelGGL((spd_paged_selected_join_kernel<T, D>), dim3((unsigned)segments), dim3(64), 0, st, a, s, c.splits, c.head_tiles);
         return hipGetLastError();
     }
     if (c.wide) {

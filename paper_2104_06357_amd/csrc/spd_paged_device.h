@@ -11,6 +11,41 @@ template <spd_dtype T> using half_t = typename Half<T>::type;
 template <spd_dtype T> using half8_t = half_t<T> __attribute__((ext_vector_type(8)));
 template <spd_dtype T> using half4_t = half_t<T> __attribute__((ext_vector_type(4)));
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+// The sum over the wavefront's lanes up to each one, itself included (row shifts, then the rows' last lanes to the rows after).
+__device__ __forceinline__ int sum_upto(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ int from_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }      // lane: the same for all
+
+// The greatest over the lanes that differ in bit 5 (of the lane's number), and in bits 4 and 5; the sum over the latter.
+__device__ __forceinline__ float greatest_of_2(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float greatest_of_4(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return greatest_of_2(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_of_2(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum_of_4(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return sum_of_2(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
 // Codes of 8 bits are multiples of the greatest magnitude times this.
 constexpr float kPagedCodeStep = 1.0f / 127.0f;
 
@@ -100,11 +135,6 @@ __device__ __forceinline__ half8_t<T> rounded(const float *x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = (half_t<T>)x[i];
     return r;
-}
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-    return (int64_t)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 
 }  // namespace spd

@@ -51,10 +51,7 @@ __device__ __forceinline__ void choose_of(int n, int k, int each, Key key, Take 
         at |= (uint64_t)(mine[j] == floor && floor > 0) << j;
     }
     const int both = __popcll(above) | __popcll(at) << 16;
-    int sum = both;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) { const int up = __shfl_up(sum, d); if (lane >= d) sum += up; }
-    const int left = k - (__shfl(sum, 63) & 0xffff), before = sum - both;
+    const int sum = sum_upto(both), left = k - (from_lane(sum, 63) & 0xffff), before = sum - both;
     int rank = (before & 0xffff) + min(before >> 16, left), more = max(0, left - (before >> 16));
     for (uint64_t rest = at; rest != 0; rest &= rest - 1, --more) if (more > 0) above |= rest & -rest;
     for (; above != 0; above &= above - 1) take(rank++, first + (int)__builtin_ctzll(above));

@@ -517,6 +517,26 @@ def test_refusals_of_the_library(spd, h):
     assert_close(w, h.paged_attention(cache, q, batch), w.attention(), "after the refusals")
 
 
+def test_scratch_of_the_callers(spd):
+    """Too little is refused and named, as much as was asked for is enough, and nothing is written past it."""
+    w = World([(300, 1), (70, 9), (9, 1)], dim=64, group=2, seed=11)
+    w.make_bounds()
+    own = spd.Handle()
+    cache, batch, q = w.cache(spd), w.batch(spd), w.queries()
+    need = own.paged_workspace_bytes(cache, batch, w.tokens, 4)
+    scratch = torch.full((need + 512,), 0x5a, dtype=torch.uint8, device="cuda")
+    at = -scratch.data_ptr() % 256
+    own.set_workspace(scratch[at:at + need // 2])
+    with pytest.raises(spd.SpdError) as e:
+        own.paged_attention(cache, q, batch)
+    assert e.value.status_name == "SPD_ERR_WORKSPACE"
+    own.set_workspace(scratch[at:at + need])
+    assert_close(w, own.paged_attention(cache, q, batch), w.attention(), "with the caller's scratch")
+    assert bool((scratch[at + need:] == 0x5a).all()) and bool((scratch[:at] == 0x5a).all())
+    own.set_workspace(None)
+    own.close()
+
+
 def test_nothing_to_do(spd, h):
     w = World([(20, 2)], dim=64)
     w.make_bounds()
