@@ -2057,7 +2057,8 @@ spd_status spd_paged_append(spd_handle *h, const spd_paged_cache *c, int64_t n_t
     spd_status st = check_paged_cache(h, c);
     if (st != SPD_OK) return st;
     if (n_tokens < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "negative number of tokens");
-    if (n_tokens >= kPagedMost) return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 tokens");
+    if (n_tokens * (int64_t)c->n_kv_heads >= kPagedMost || n_tokens >= kPagedMost)
+        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 rows (tokens x heads)");
     if (n_tokens == 0) return SPD_OK;
     if (!slots) return fail(h, SPD_ERR_NULL, "slots is NULL");
     if ((st = check_paged_rows(h, k_new, "k_new")) != SPD_OK || (st = check_paged_rows(h, v_new, "v_new")) != SPD_OK) return st;

@@ -120,10 +120,10 @@ __global__ void __launch_bounds__(kAppendRows * D / 8) spd_paged_append_kernel(c
     constexpr int kLanes = D / 8;
     __shared__ int64_t s_slot[kAppendRows];
     __shared__ int32_t s_run[kAppendRows];                        // the row of the window at which the row's run begins; -1: before the window, or no slot
-    __shared__ __align__(16) float s_lo[2][kAppendRows][D], s_hi[2][kAppendRows][D];      // of the window's rows, and of those past it
+    __shared__ __align__(16) H s_lo[2][kAppendRows][D], s_hi[2][kAppendRows][D];          // of the window's rows, and of those past it
     __shared__ int32_t s_past;                                    // rows past the window that its last run has
-    const int tid = (int)threadIdx.x, row = tid / kLanes, part = tid % kLanes, head = (int)blockIdx.y;
-    const int64_t t0 = (int64_t)blockIdx.x * kAppendRows, page = (int64_t)1 << a.shift, most = a.c.n_pages << a.shift;
+    const int tid = (int)threadIdx.x, row = tid / kLanes, part = tid % kLanes, head = (int)(blockIdx.x % (unsigned)a.c.n_kv_heads);
+    const int64_t t0 = (int64_t)(blockIdx.x / (unsigned)a.c.n_kv_heads) * kAppendRows, page = (int64_t)1 << a.shift, most = a.c.n_pages << a.shift;
     if (tid < 64) {                                               // the first wavefront: a row to a lane, the window's and those after it
         int64_t t = t0 + tid, slot = t < a.n_tokens ? a.slots[t] : -1;
         const bool real = slot >= 0 && slot < most;
@@ -155,17 +155,19 @@ __global__ void __launch_bounds__(kAppendRows * D / 8) spd_paged_append_kernel(c
     const H *const k_new = (const H *)a.k_new.ptr + head * a.k_new.head_stride + part * 8;
     const H *const v_new = (const H *)a.v_new.ptr + head * a.v_new.head_stride + part * 8;
     float lo[8], hi[8];
-    auto move = [&](int64_t t, int64_t slot) {
-        const H8 k = *(const H8 *)(k_new + t * a.k_new.token_stride), v = *(const H8 *)(v_new + t * a.v_new.token_stride);
+    auto move = [&](int64_t slot, H8 k, H8 v) {
         const int64_t to = (slot >> a.shift) * a.c.page_stride + (slot & (page - 1)) * a.c.token_stride + cache_at;
         *(H8 *)((H *)a.c.k + to) = k;
         *(H8 *)((H *)a.c.v + to) = v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], (float)k[e]); hi[e] = fmaxf(hi[e], (float)k[e]); }
     };
-    auto keep = [&](int which) {
+    auto keep = [&](int which) {                                  // (they are values of the cache's type)
+        H8 l, h;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { s_lo[which][row][part * 8 + e] = lo[e]; s_hi[which][row][part * 8 + e] = hi[e]; }
+        for (int e = 0; e < 8; ++e) { l[e] = (H)lo[e]; h[e] = (H)hi[e]; }
+        *(H8 *)&s_lo[which][row][part * 8] = l;
+        *(H8 *)&s_hi[which][row][part * 8] = h;
     };
     auto forget = [&] {
 #pragma unroll
@@ -173,15 +175,31 @@ __global__ void __launch_bounds__(kAppendRows * D / 8) spd_paged_append_kernel(c
     };
     auto join = [&](int which, int i) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], s_lo[which][i][part * 8 + e]); hi[e] = fmaxf(hi[e], s_hi[which][i][part * 8 + e]); }
+        for (int e = 0; e < 8; ++e) { lo[e] = fminf(lo[e], (float)s_lo[which][i][part * 8 + e]); hi[e] = fmaxf(hi[e], (float)s_hi[which][i][part * 8 + e]); }
     };
     const int run = s_run[row], last = s_run[kAppendRows - 1], past = s_past;
     forget();
-    if (run >= 0) move(t0 + row, s_slot[row]);
+    if (run >= 0) {
+        const int64_t t = t0 + row;
+        move(s_slot[row], *(const H8 *)(k_new + t * a.k_new.token_stride), *(const H8 *)(v_new + t * a.v_new.token_stride));
+    }
     keep(0);
     if (past > 0) {                                               // all rows' lanes together
         forget();
-        for (int i = row; i < past; i += kAppendRows) move(t0 + kAppendRows + i, s_slot[kAppendRows - 1] + 1 + i);
+        for (int i0 = row; i0 < past; i0 += 4 * kAppendRows) {    // four rows of a lane are on their way at a time
+            H8 k[4], v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t t = t0 + kAppendRows + min(i0 + j * kAppendRows, past - 1);
+                k[j] = *(const H8 *)(k_new + t * a.k_new.token_stride);
+                v[j] = *(const H8 *)(v_new + t * a.v_new.token_stride);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = i0 + j * kAppendRows;
+                if (i < past) move(s_slot[kAppendRows - 1] + 1 + i, k[j], v[j]);
+            }
+        }
         keep(1);
     }
     if (a.c.bounds == nullptr) return;
@@ -239,7 +257,8 @@ hipError_t launch_paged_append(hipStream_t st, const spd_paged_cache &c, int64_t
                                const spd_rows &v_new, const int64_t *slots) {
     if (n_tokens == 0) return hipSuccess;
     AppendArgs a{c, n_tokens, k_new, v_new, slots, __builtin_ctz((unsigned)c.page_size)};
-    const dim3 grid((unsigned)((n_tokens + kAppendRows - 1) / kAppendRows), (unsigned)c.n_kv_heads);
+    // heads next to each other: a token's rows lie together
+    const dim3 grid((unsigned)((n_tokens + kAppendRows - 1) / kAppendRows * c.n_kv_heads));
     const dim3 block((unsigned)(kAppendRows * c.head_dim / 8));
     if (c.dtype == SPD_BF16) {
         if (c.head_dim == 64) hipLaunchKernelGGL((spd_paged_append_kernel<SPD_BF16, 64>), grid, block, 0, st, a);

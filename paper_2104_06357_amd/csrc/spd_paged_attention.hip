@@ -98,18 +98,21 @@ __global__ void __launch_bounds__(kScheduleThreads) spd_paged_schedule_kernel(co
 }
 
 // The share of worker `w` of `workers` in `all` units.
-__device__ __forceinline__ int64_t share_begin(int64_t all, int64_t workers, int64_t w) {
+template <typename Int>             // (the narrow kernels count in 32 bits: a division of 64 takes a third of a microsecond)
+__device__ __forceinline__ Int share_begin(Int all, Int workers, Int w) {
     return all / workers * w + min(w, all % workers);
 }
 
 // The worker who has unit `x`.
-__device__ __forceinline__ int64_t worker_of(int64_t all, int64_t workers, int64_t x) {
-    const int64_t each = all / workers, more = all % workers;
-    return x < (each + 1) * more ? x / (each + 1) : more + (x - (each + 1) * more) / max(each, (int64_t)1);
+template <typename Int>
+__device__ __forceinline__ Int worker_of(Int all, Int workers, Int x) {
+    const Int each = all / workers, more = all % workers;
+    return x < (each + 1) * more ? x / (each + 1) : more + (x - (each + 1) * more) / max(each, (Int)1);
 }
 
 // As many workers as there are, but no fewer than `least` units to one.
-__device__ __forceinline__ int64_t workers_for(int64_t all, int64_t workers, int64_t least) { return max((int64_t)1, min(workers, all / least)); }
+template <typename Int>
+__device__ __forceinline__ Int workers_for(Int all, Int workers, Int least) { return max((Int)1, min(workers, all / least)); }
 
 struct Place { int64_t segment_begin; int tile, head; };        // segment_begin: its first unit's number
 
@@ -199,7 +202,7 @@ struct Narrow {
         if (SELECTED) {
             const int32_t *const list = a.selected + ((int64_t)p.first_token * a.cache.kv_heads + p.head) * a.n_select;
             if (lane < a.n_select) chosen = list[lane];
-            if (chosen >= 0) chosen_number = table[chosen];
+            if (chosen >= 0 && chosen < a.req.max_pages) chosen_number = table[chosen];
         } else {
             pages.begin(table, a.req.max_pages, (p.unit0 * 2) >> per_page);
         }
@@ -405,29 +408,32 @@ __device__ __forceinline__ NarrowPart narrow_part(const PagedAttention &a, const
 }
 
 // Where the workers' shares begin and end: every wavefront counts the tiles and units itself, a request to a lane, instead
-// of waiting for another kernel to do it.  (The host takes care that a key head's units are fewer than 2^31.)
+// of waiting for another kernel to do it.  (The host takes care that there are fewer than 2^31 units.)
 struct Counted {
     const PagedAttention *a;
     int32_t per_head, tiles;            // units and tiles
     PagedRequest rq;                    // the lane's request, of the last 64 that were counted
     int32_t upto;                       // units of the requests up to it
+    bool descends;                      // query_start does somewhere: requests would overlap, and be more than the host counted on
 
     __device__ __forceinline__ int count(int base, int before) {
         const int r = base + ((int)threadIdx.x & 63);
         int many = 0, u = 0;
         if (r < a->req.n_requests) {
             rq = paged_request(a->req, a->cache.page_shift, r);
+            descends |= a->req.query_start[r + 1] < a->req.query_start[r];
             many = (rq.count * a->q.group + kNarrowRows - 1) / kNarrowRows;
             for (int i = 0; i < many; ++i) u += tile_units(rq, a->q.group, kNarrowRows, kNarrowKeys, i);
         }
         upto = before + sum_upto(u);
         return many;
     }
-    __device__ __forceinline__ explicit Counted(const PagedAttention &args) : a(&args), per_head(0), tiles(0), rq{0, 0, 0}, upto(0) {
+    __device__ __forceinline__ explicit Counted(const PagedAttention &args) : a(&args), per_head(0), tiles(0), rq{0, 0, 0}, upto(0), descends(false) {
         for (int base = 0; base < a->req.n_requests; base += 64) {
             tiles += from_lane(sum_upto(count(base, per_head)), 63);
             per_head = from_lane(upto, 63);
         }
+        if (__any(descends)) per_head = tiles = 0;
     }
     __device__ __forceinline__ PagedRequest request(int r) const {
         if (a->req.n_requests > 64) return paged_request(a->req, a->cache.page_shift, r);
@@ -439,17 +445,17 @@ struct Counted {
 struct Cursor {
     PagedRequest rq;
     int request, tile, tiles, head;
-    int64_t begin;                      // the segment's first unit
+    uint32_t begin;                     // the segment's first unit
     __device__ __forceinline__ void enter(const Counted &c, int r) {
         request = uniform(r);
         rq = c.request(request);
         tiles = (rq.count * c.a->q.group + kNarrowRows - 1) / kNarrowRows;
         tile = 0;
     }
-    __device__ __forceinline__ int units(const Counted &c) const { return tile_units(rq, c.a->q.group, kNarrowRows, kNarrowKeys, tile); }
-    __device__ __forceinline__ void find(Counted &c, int64_t at) {
-        head = uniform((int)(at / c.per_head));
-        const int64_t start = (int64_t)head * c.per_head;
+    __device__ __forceinline__ uint32_t units(const Counted &c) const { return tile_units(rq, c.a->q.group, kNarrowRows, kNarrowKeys, tile); }
+    __device__ __forceinline__ void find(Counted &c, uint32_t at) {
+        head = uniform((int)(at / (uint32_t)c.per_head));
+        const uint32_t start = (uint32_t)head * (uint32_t)c.per_head;
         const int x = (int)(at - start);
         for (int base = 0, before = 0;; base += 64) {
             if (c.a->req.n_requests > 64) c.count(base, before);
@@ -462,9 +468,9 @@ struct Cursor {
             }
             before = to;
         }
-        for (int u = units(c); at >= begin + u; u = units(c)) { begin += u; ++tile; }
+        for (uint32_t u = units(c); at >= begin + u; u = units(c)) { begin += u; ++tile; }
     }
-    __device__ __forceinline__ void next(const Counted &c, int units) {
+    __device__ __forceinline__ void next(const Counted &c, uint32_t units) {
         begin += units;
         if (++tile < tiles) return;
         int r = request;
@@ -474,7 +480,7 @@ struct Cursor {
 
 // Workers are whole workgroups where segments are long (a part's sums are then joined in LDS, a quarter as many go through scratch), and
 // wavefronts of their own where they are short (no wavefront waits for others).
-constexpr int kLongSegment = 16, kNarrowLeast = 2;      // units; of a wavefront at the least, since each more part is more to join
+constexpr int kLongSegment = 16, kNarrowLeast = 1;      // units; of a wavefront at the least, since each more part is more to join
 
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(const PagedAttention a, const Schedule s) {
@@ -483,28 +489,28 @@ __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(
     const int wave = uniform((int)threadIdx.x >> 6);
     Counted counted(a);
     const int team = counted.per_head / kLongSegment >= counted.tiles ? kNarrowWaves : 1, me = team == 1 ? 0 : wave;
-    const int64_t all = (int64_t)counted.per_head * a.cache.kv_heads;
-    const int64_t workers = workers_for(all, (int64_t)gridDim.x * kNarrowWaves / team, kNarrowLeast * team);
+    const uint32_t all = (uint32_t)counted.per_head * (uint32_t)a.cache.kv_heads;
+    const uint32_t workers = workers_for(all, gridDim.x * kNarrowWaves / team, (uint32_t)(kNarrowLeast * team));
     // neighbours in the units' order share an XCD and its L2 (workgroups go to the XCDs in turn)
-    const int64_t group = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = team == 1 ? group * kNarrowWaves + wave : group;
-    int64_t at = w < workers ? share_begin(all, workers, w) : all;
-    const int64_t end = w < workers ? share_begin(all, workers, w + 1) : all;
+    const uint32_t group = (blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8, w = team == 1 ? group * kNarrowWaves + wave : group;
+    uint32_t at = w < workers ? share_begin(all, workers, w) : all;
+    const uint32_t end = w < workers ? share_begin(all, workers, w + 1) : all;
     Joined joined{};
     Cursor c;
     if (at < end) c.find(counted, at);
     while (at < end) {
-        const int units = c.units(counted), unit0 = uniform((int)(at - c.begin)), unit1 = uniform((int)min((int64_t)units, end - c.begin));
+        const uint32_t units = c.units(counted), unit0 = at - c.begin, unit1 = min(units, end - c.begin);
         NarrowPart p = narrow_part(a, c.rq, c.request, c.tile * kNarrowRows, c.head);
-        p.unit0 = unit0; p.unit1 = unit1;
-        if (team > 1) {
-            p.unit0 = unit0 + (int)((uint32_t)(unit1 - unit0) * (uint32_t)me / kNarrowWaves);
-            p.unit1 = unit0 + (int)((uint32_t)(unit1 - unit0) * (uint32_t)(me + 1) / kNarrowWaves);
+        p.unit0 = uniform((int)unit0); p.unit1 = uniform((int)unit1);
+        if (team > 1) {                 // (fewer than 2^27 units to a segment)
+            p.unit0 = uniform((int)(unit0 + (unit1 - unit0) * (uint32_t)me / kNarrowWaves));
+            p.unit1 = uniform((int)(unit0 + (unit1 - unit0) * (uint32_t)(me + 1) / kNarrowWaves));
         }
         Narrow<T, D, false> n;
         if (p.unit0 < p.unit1) n.walk(a, p, s_kv[wave]); else n.clear();
         if (team > 1) n.template join_team<kNarrowWaves>([&](int i) { return s_kv[i]; }, s_stats, me);
         if (unit0 == 0 && unit1 == units) n.write(a, p, team, me);
-        else n.leave(s, 2 * w + (unit0 == 0 ? 1 : 0), team, me);
+        else n.leave(s, 2 * (int64_t)w + (unit0 == 0 ? 1 : 0), team, me);
         if (unit0 == 0 && unit1 < units)
             joined = Joined{(int)(worker_of(all, workers, c.begin + units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, (int)w};
         at = c.begin + unit1;
@@ -576,8 +582,8 @@ __global__ void __launch_bounds__((TEAM == 1 ? kNarrowWaves : TEAM) * 64, 2)
     NarrowPart p;
     int units;
     if (!selected_part(a, w / splits, head_tiles, p, units)) return;
-    p.unit0 = uniform((int)share_begin(units, (int64_t)splits * TEAM, split));
-    p.unit1 = uniform((int)share_begin(units, (int64_t)splits * TEAM, split + 1));
+    p.unit0 = uniform((int)share_begin(units, splits * TEAM, split));
+    p.unit1 = uniform((int)share_begin(units, splits * TEAM, split + 1));
     Narrow<T, D, true> n;
     if (p.unit0 < p.unit1) n.walk(a, p, s_kv[wave]); else n.clear();
     if (TEAM > 1) n.template join_team<TEAM>([&](int i) { return s_kv[i]; }, s_stats, me);
@@ -824,7 +830,7 @@ __global__ void __launch_bounds__(kWideWaves * 64, 2) spd_paged_wide_kernel(cons
     __shared__ __align__(16) half_t<T> s_kv[4 * kWideKeys * D];
     const int n_tiles = s.n_tiles[0];
     const int64_t w = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-    const int64_t per_head = n_tiles ? s.first[n_tiles] : 0, all = per_head * a.cache.kv_heads, workers = workers_for(all, gridDim.x, kWideLeast);
+    const int64_t per_head = n_tiles ? s.first[n_tiles] : 0, all = per_head * a.cache.kv_heads, workers = workers_for(all, (int64_t)gridDim.x, kWideLeast);
     int64_t at = w < workers ? share_begin(all, workers, w) : all;
     const int64_t end = w < workers ? share_begin(all, workers, w + 1) : all;
     Joined joined{};
@@ -884,15 +890,18 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
         c.head_tiles = (a.q.group + kNarrowRows - 1) / kNarrowRows;
         const int64_t segments = std::max<int64_t>(1, (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles);
         const int64_t units = ((int64_t)a.n_select << a.cache.page_shift) / kNarrowKeys;
-        c.team = segments >= (int64_t)n_cus * 8 ? 1 : kSelectedTeam;
+        // In units of a wavefront, with what a segment costs beside them (10): 1,964 segments of 13 units took 25 us in teams and 19 by
+        // wavefronts, 256 of 64 units 43 and 57.
+        const int64_t rounds_of_teams = (segments + n_cus - 1) / n_cus, rounds_of_waves = (segments + n_cus * 8 - 1) / (n_cus * 8);
+        c.team = rounds_of_teams * (10 + units / kSelectedTeam) < rounds_of_waves * (10 + units) ? kSelectedTeam : 1;
         // up to 8 units of a wavefront cost less than a second launch that joins (4 us)
         c.splits = c.team == 1 ? 1 : (int)std::max<int64_t>(1, std::min(units / (kSelectedTeam * 8), n_cus / segments));
         c.workers = 0;
         return c;
     }
     // A wavefront of the narrow kernel counts the units itself, 64 requests at a time and in 32 bits.
-    const int64_t most_units = (rows / kNarrowRows + a.req.n_requests) * ((((int64_t)a.req.max_pages << a.cache.page_shift) + kNarrowKeys - 1) / kNarrowKeys + 1);
-    c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256 || most_units >= (int64_t)1 << 31;
+    const double most_units = (double)(rows / kNarrowRows + a.req.n_requests) * (double)((((int64_t)a.req.max_pages << a.cache.page_shift) + kNarrowKeys - 1) / kNarrowKeys + 1);
+    c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256 || most_units * a.cache.kv_heads >= 2147483648.0;
     c.rows = c.wide ? kWideRows : kNarrowRows;
     c.keys = c.wide ? kWideKeys : kNarrowKeys;
     c.threads = c.wide ? kWideWaves * 64 : 64;
