@@ -156,6 +156,15 @@ def test_append_in_steps_of_any_size(spd, h, dtype, dim, layout, page):
     check_append(spd, h, w, [[(r, n) for r, (_, n) in enumerate(w.requests)]], dtype)
 
 
+@pytest.mark.parametrize("dim,page,heads", [(128, 64, 4), (64, 16, 3), (64, 1024, 5)])
+def test_append_of_long_prompts(spd, h, dim, page, heads):
+    """Rows enough for the windows of 64, pages that begin anywhere in them, runs that go on past several."""
+    n = 66_000 // heads
+    w = World([(0, n // 2 + 5), (0, 3), (0, n // 2 + 777), (0, 40)], dim=dim, page=page, kv_heads=heads, seed=dim)
+    print("append", dim, page, heads, flush=True)
+    check_append(spd, h, w, [[(0, 7), (2, 777), (3, 1)], [(0, n // 2 - 2), (1, 3), (2, n // 2), (3, 39)]], "bf16")
+
+
 def test_append_token_by_token(spd, h):
     w = World([(0, 40), (0, 21)], page=16, seed=4)
     check_append(spd, h, w, [[(0, 1), (1, 1 if i < 21 else 0)] for i in range(40)], "bf16")
