@@ -155,7 +155,7 @@ struct Pages {
 
 // ---- few rows: a wavefront to 16 of them --------------------------------------------------------
 // Decoding, and selected pages: one to 16 rows, and every key is read once.  A wavefront is a worker of its own, and no barrier is in its
-// loop: 32 keys a unit, through 16 KB of LDS, from where V is read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
+// loop: 32 keys a unit, through 8 KB of LDS, K before V, from where V is read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
 // lanes and order in which the second takes them, and a row is a lane's, its statistics too.
 
 constexpr int kNarrowRows = 16, kNarrowKeys = 32, kNarrowWaves = 4;
@@ -224,17 +224,14 @@ struct Narrow {
         // (a row's chunks go to neighbouring lanes, which memory answers four at a time; the products' order, a row to a lane, is made by LDS)
         const int l_row = lane / kChunks, l_chunk = lane % kChunks;
         const uint32_t l_at = (uint32_t)l_row * (uint32_t)a.cache.token_stride * 2 + (uint32_t)l_chunk * 16;
-        auto fetch = [&](const int *ok, const int64_t *at) {
+        auto fetch = [&](H8 *to, const void *from, const int *ok, const int64_t *at) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (!ok[j]) continue;
-                const char *const k = (const char *)a.cache.k + uniform(at[j]) * 2, *const v = (const char *)a.cache.v + uniform(at[j]) * 2;
+                const char *const p = (const char *)from + uniform(at[j]) * 2;
 #pragma unroll
-                for (int i = 0; i < kLoads / 2; ++i) {
-                    const int64_t more = (int64_t)(i * kRowsOfLoad) * a.cache.token_stride * 2;
-                    kr[j * (kLoads / 2) + i] = *(const H8 *)(k + more + l_at);
-                    vr[j * (kLoads / 2) + i] = *(const H8 *)(v + more + l_at);
-                }
+                for (int i = 0; i < kLoads / 2; ++i)
+                    to[j * (kLoads / 2) + i] = *(const H8 *)(p + (int64_t)(i * kRowsOfLoad) * a.cache.token_stride * 2 + l_at);
             }
         };
         H8 zero;
@@ -242,33 +239,40 @@ struct Narrow {
         for (int i = 0; i < 8; ++i) zero[i] = (H)0.0f;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) kr[i] = vr[i] = zero;
-        const LdsBytes s_k = lds_bytes(lds), s_v = s_k + kNarrowKeys * D * 2;
-        const int s = lane & 15, k_lane = k_at<D>(row, quad), v_lane = v_at<D>(quad * 4 + (s >> 2), (s & 3) >> 1) + (s & 1) * 8;
+        // (one tile of LDS: K until the first product has read it, then V)
+        const LdsBytes tile = lds_bytes(lds);
+        const int s = lane & 15, k_lane = k_at<D>(row, quad), v_lane = v8_at<D>(quad * 4 + (s >> 2), (s & 3) >> 1) + (s & 1) * 8;
         locate(p.unit0, pos0, here, base);
-        fetch(here, base);
+        fetch(kr, a.cache.k, here, base);
+        fetch(vr, a.cache.v, here, base);
         for (int u = p.unit0; u < p.unit1; ++u) {
             int pos_next[2] = {0, 0}, here_next[2] = {0, 0};
             int64_t base_next[2] = {0, 0};
             if (u + 1 < p.unit1) locate(u + 1, pos_next, here_next, base_next);
-            // into LDS; values that no row of the tile sees become 0, since 0 times what lies there need not be
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int j = i / (kLoads / 2), r = (i % (kLoads / 2)) * kRowsOfLoad + l_row;
-                write_row<T>(s_k + k_at<D>(j * 16 + r, l_chunk), kr[i]);
-                if (!here[j] || pos0[j] + 15 > most) { if (!here[j] || pos0[j] + r > most) vr[i] = zero; }
-                write_row<T>(s_v + v_at<D>(j * 16 + r, l_chunk), vr[i]);
+                write_row<T>(tile + k_at<D>(j * 16 + r, l_chunk), kr[i]);
             }
+            fetch(kr, a.cache.k, here_next, base_next);
             f32x4 x[2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                x[j] = f32x4{0, 0, 0, 0};
+            for (int j = 0; j < 2; ++j) x[j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) x[j] = mfma16(read_row<T>(s_k + (k_lane ^ (s << 6)) + j * 32 * D), q[s], x[j]);
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) x[j] = mfma16(read_row<T>(tile + (k_lane ^ (s << 6)) + j * 32 * D), q[s], x[j]);
+            // values that no row of the tile sees become 0, since 0 times what lies there need not be
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int j = i / (kLoads / 2), r = (i % (kLoads / 2)) * kRowsOfLoad + l_row;
+                if (!here[j] || pos0[j] + 15 > most) { if (!here[j] || pos0[j] + r > most) vr[i] = zero; }
+                write_row<T>(tile + v8_at<D>(j * 16 + r, l_chunk), vr[i]);
             }
             const int now_pos[2] = {pos0[0], pos0[1]}, now_here[2] = {here[0], here[1]};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) { pos0[j] = pos_next[j]; here[j] = here_next[j]; base[j] = base_next[j]; }
-            fetch(here, base);
+            for (int j = 0; j < 2; ++j) { pos0[j] = pos_next[j]; here[j] = here_next[j]; }
+            fetch(vr, a.cache.v, here_next, base_next);
             // weights, a row's keys 4 quad + i of either step
             float w[8];
 #pragma unroll
@@ -295,7 +299,7 @@ struct Narrow {
             for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(w[i], a.q.scale, -from)); sum += w[i]; }
             const H8 pw = rounded<T>(w);
 #pragma unroll
-            for (int d = 0; d < kDims; ++d) o[d] = mfma16(read_transposed<T>(s_v + (v_lane ^ (d << 5)), 32 * D), pw, o[d]);
+            for (int d = 0; d < kDims; ++d) o[d] = mfma16(read_transposed<T>(tile + (v_lane ^ (d << 5)), 32 * D), pw, o[d]);
         }
         sum = sum_of_4(sum);
     }
@@ -484,7 +488,7 @@ constexpr int kLongSegment = 16, kNarrowLeast = 1;      // units; of a wavefront
 
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(const PagedAttention a, const Schedule s) {
-    __shared__ __align__(16) half_t<T> s_kv[kNarrowWaves][2 * kNarrowKeys * D];
+    __shared__ __align__(16) half_t<T> s_kv[kNarrowWaves][kNarrowKeys * D];
     __shared__ float2 s_stats[kNarrowWaves][64];
     const int wave = uniform((int)threadIdx.x >> 6);
     Counted counted(a);
@@ -568,10 +572,10 @@ __device__ __forceinline__ bool selected_part(const PagedAttention &a, int64_t s
 }
 
 template <spd_dtype T, int D, int TEAM>
-__global__ void __launch_bounds__((TEAM == 1 ? kNarrowWaves : TEAM) * 64, 2)
+__global__ void __launch_bounds__((TEAM == 1 ? kNarrowWaves : TEAM) * 64, TEAM == 1 ? 3 : 2)
     spd_paged_selected_kernel(const PagedAttention a, const Schedule s, const int splits, const int head_tiles) {
     constexpr int kWaves = TEAM == 1 ? kNarrowWaves : TEAM;
-    __shared__ __align__(16) half_t<T> s_kv[kWaves][2 * kNarrowKeys * D];
+    __shared__ __align__(16) half_t<T> s_kv[kWaves][kNarrowKeys * D];
     __shared__ float2 s_stats[TEAM == 1 ? 1 : TEAM][64];
     const int wave = uniform((int)threadIdx.x >> 6), me = TEAM == 1 ? 0 : wave;
     // (a token's and its neighbours' segments share pages: neighbours share an XCD)

@@ -125,8 +125,9 @@ __device__ __forceinline__ half8_t<T> read_transposed(LdsBytes p, int apart) {
 }
 
 // Where 16-byte chunk c of row r lies in a tile of K, read a chunk of many rows at a time, and of V, read transposed, 4 rows by 64
-// bytes: such rows in different banks.
+// bytes or (v8_at) 8 rows by 32: such rows in different banks.
 template <int D> __device__ __forceinline__ int k_at(int r, int c) { return r * D * 2 + (D == 128 ? (c ^ (r & 15)) : (c ^ ((r >> 1) & 7))) * 16; }
+template <int D> __device__ __forceinline__ int v8_at(int r, int c) { return r * D * 2 + (D == 128 ? (c ^ ((r & 7) << 1)) : (c ^ (((r >> 1) & 3) << 1))) * 16; }
 template <int D> __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + (D == 128 ? (c ^ ((r & 3) << 2)) : (c ^ (((r >> 1) & 1) << 2))) * 16; }
 
 template <spd_dtype T>
