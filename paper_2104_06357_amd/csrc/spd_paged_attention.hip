@@ -622,6 +622,7 @@ struct Wide {
     static constexpr int kChunks = D / 8, kSteps = D / 16, kDims = D / 32;
     static constexpr int kThreads = kWideWaves * 64, kRowsOfLoad = kThreads / kChunks, kLoads = kWideKeys / kRowsOfLoad;
     static constexpr int kTile = kWideKeys * D * 2;     // bytes of K or V in LDS
+    static constexpr int kAhead = 4;                    // reads of LDS that are on their way
 
     H8 q[kSteps];
     f32x16 o[kDims];
@@ -703,16 +704,26 @@ struct Wide {
             f32x16 x[2];
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.0f;
+            // (in this order: a read of LDS is on its way while four products are taken)
+            auto key_rows = [&](int i) { return read_row<T>(k + (k_lane ^ ((i >> 1) << 5)) + (i & 1) * 64 * D); };
+            H8 ahead[kAhead];
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
+            for (int i = 0; i < kAhead; ++i) ahead[i] = key_rows(i);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < 2; ++t) x[t] = mfma32(read_row<T>(k + (k_lane ^ (s << 5)) + t * 64 * D), q[s], x[t]);
+            for (int i = 0; i < 2 * kSteps; ++i) {
+                x[i & 1] = mfma32(ahead[i % kAhead], q[i >> 1], x[i & 1]);
+                if (i + kAhead < 2 * kSteps) ahead[i % kAhead] = key_rows(i + kAhead);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             if (edge) {
                 asm volatile("");                       // (a branch: few units have one)
+                const int last = position - key0 - half * 4;        // of the row's keys of this unit, counted from the lane's first
+                const uint64_t seen = there >> (half * 4);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    const int c = (i >> 4) * 32 + ((i & 15) >> 2) * 8 + half * 4 + (i & 3);
-                    if (key0 + c > position || !((there >> c) & 1)) x[i >> 4][i & 15] = -__builtin_inff();
+                    const int c = (i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3);
+                    if (c > last || !((seen >> c) & 1)) x[i >> 4][i & 15] = -__builtin_inff();
                 }
             }
             float big = x[0][0];
@@ -729,16 +740,28 @@ struct Wide {
                     for (int i = 0; i < 16; ++i) o[d][i] *= old;
             }
             const float from = top == -__builtin_inff() ? 0.0f : top;
+            // the weights of 16 keys, then their products beside the weights of the next 16
+            auto values = [&](int i) { return read_transposed<T>(k + (v_lane ^ ((i % kDims) << 6)) + (i / kDims) * 32 * D, 16 * D); };
+            float w[8];
+            auto weigh = [&](int e, int first, int many) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {               // 16 keys
-                float w[8];
+                for (int i = first; i < first + many; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(x[e >> 1][(e & 1) * 8 + i], a.q.scale, -from)); sum += w[i]; }
+            };
 #pragma unroll
-                for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(x[e >> 1][(e & 1) * 8 + i], a.q.scale, -from)); sum += w[i]; }
-                const H8 pw = rounded<T>(w);
+            for (int i = 0; i < kAhead; ++i) ahead[i] = values(i);
+            __builtin_amdgcn_sched_barrier(0);
+            weigh(0, 0, 8);
+            H8 pw = rounded<T>(w);
 #pragma unroll
-                for (int d = 0; d < kDims; ++d)
-                    o[d] = mfma32(read_transposed<T>(k + (v_lane ^ (d << 6)) + e * 32 * D, 16 * D), pw, o[d]);
+            for (int i = 0; i < 4 * kDims; ++i) {
+                const int e = i / kDims, d = i % kDims;
+                __builtin_amdgcn_sched_barrier(0);
+                o[d] = mfma32(ahead[i % kAhead], pw, o[d]);
+                if (i + kAhead < 4 * kDims) ahead[i % kAhead] = values(i + kAhead);
+                if (e < 3) weigh(e + 1, d * (8 / kDims), 8 / kDims);
+                if (e < 3 && d + 1 == kDims) pw = rounded<T>(w);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
         // Unit u is in LDS while u + 1 and u + 2 are on their way in registers: memory has the time of two units to answer.
         Loaded odd, even;
