@@ -1763,8 +1763,8 @@ spd_status check_paged_cache(spd_handle *h, const spd_paged_cache *c) {
     if (c->n_pages > 0 && (!c->k || !c->v)) return fail(h, SPD_ERR_NULL, "k or v of the cache is NULL");
     if (((c->page_stride | c->token_stride | c->head_stride) & 7) != 0 || !aligned16(c->k) || !aligned16(c->v))
         return fail(h, SPD_ERR_UNSUPPORTED, "strides of the cache must be multiples of 8 elements, k and v 16-byte aligned");
-    if (c->token_stride < 0 || c->token_stride >= ((int64_t)1 << 26))
-        return fail(h, SPD_ERR_UNSUPPORTED, "token_stride of the cache must lie below 2^26 elements");
+    if (c->page_stride < 0 || c->head_stride < 0 || c->token_stride < 0 || c->token_stride >= ((int64_t)1 << 26))
+        return fail(h, SPD_ERR_UNSUPPORTED, "strides of the cache must not be negative, token_stride below 2^26 elements");
     if ((c->bounds != nullptr) != (c->codes != nullptr) || (c->bounds != nullptr) != (c->code_scale != nullptr))
         return fail(h, SPD_ERR_NULL, "bounds, codes and code_scale of the cache go together");
     if (!aligned16(c->bounds) || !aligned16(c->codes)) return fail(h, SPD_ERR_UNSUPPORTED, "bounds and codes must be 16-byte aligned");
@@ -1818,6 +1818,10 @@ spd_status run_paged(spd_handle *h, const spd_paged_cache *c, const spd_paged_ba
     a.q.token_stride = q->token_stride;
     a.q.head_stride = q->head_stride;
     a.q.scale = scale * 1.4426950408889634f;
+    if (c->n_pages == 0) {                                  // (kernels read some row where there is none to see)
+        a.cache.k = a.cache.v = q->ptr;
+        a.cache.page_stride = a.cache.token_stride = a.cache.head_stride = 0;
+    }
     a.out = PagedOut{out, lse};
     a.selected = selected;
     a.n_select = n_select;

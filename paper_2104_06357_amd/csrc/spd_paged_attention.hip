@@ -153,6 +153,38 @@ struct Pages {
     }
 };
 
+// The same as the places of the pages in memory, worked out by the lanes for 64 pages together: a unit's are then read from a lane.
+struct PagePlaces {
+    const int32_t *list;
+    const PagedCache *cache;
+    int n, block, after;
+    int64_t head_at;                    // bytes, of the key head
+    uint32_t low, high;                 // bytes, of the lane's page
+    uint64_t there;                     // whose pages there are
+    __device__ __forceinline__ int load(int b) const {
+        const int i = b * 64 + ((int)threadIdx.x & 63);
+        return i < n ? list[i] : -1;
+    }
+    __device__ __forceinline__ void place(int number) {
+        there = __ballot(number >= 0 && number < cache->n_pages);
+        const int64_t at = (int64_t)number * cache->page_stride * 2 + head_at;
+        low = (uint32_t)at; high = (uint32_t)((uint64_t)at >> 32);
+    }
+    __device__ __forceinline__ void begin(const PagedCache &c, const int32_t *l, int many, int head, int at) {
+        list = l; cache = &c; n = many; block = at >> 6;
+        head_at = (int64_t)head * c.head_stride * 2;
+        const int now = load(block);
+        after = load(block + 1);
+        place(now);
+    }
+    __device__ __forceinline__ void go(int i) {         // i: uniform, not descending
+        if ((i >> 6) != block) { block = i >> 6; place(after); after = load(block + 1); }
+    }
+    __device__ __forceinline__ int64_t at(int i) const {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, i & 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, i & 63));
+    }
+};
+
 // ---- few rows: a wavefront to 16 of them --------------------------------------------------------
 // Decoding, and selected pages: one to 16 rows, and every key is read once.  A wavefront is a worker of its own, and no barrier is in its
 // loop: 32 keys a unit, through 8 KB of LDS, K before V, from where V is read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
@@ -652,42 +684,45 @@ struct Wide {
         const bool busy = wave * 32 < p.rows;           // this wavefront has rows
         const int least = p.position0 + (p.row0 + min(wave * 32, p.rows - 1)) / a.q.group,
                   most = p.position0 + (p.row0 + min(wave * 32 + 31, p.rows - 1)) / a.q.group;
-        Pages pages;
-        pages.begin(a.req.block_table + (int64_t)p.request * a.req.table_stride, a.req.max_pages, (p.unit0 * kWideKeys) >> shift);
+        PagePlaces pages;
+        pages.begin(a.cache, a.req.block_table + (int64_t)p.request * a.req.table_stride, a.req.max_pages, p.head, (p.unit0 * kWideKeys) >> shift);
         const int l_row = tid / kChunks, l_chunk = tid % kChunks;
         const uint32_t l_at = (uint32_t)(l_row & 15) * (uint32_t)a.cache.token_stride * 2 + (uint32_t)l_chunk * 16;
         H8 zero;
 #pragma unroll
         for (int i = 0; i < 8; ++i) zero[i] = (H)0.0f;
-        struct Loaded { H8 k[kLoads], v[kLoads]; uint64_t there; };     // of a unit; there: keys whose page is there
+        // Every fetch is as many loads, whatever there is to see, so that the wait for a unit's is not one for the next one's too: what is not to be seen
+        // is read from the cache's first rows, and V of it becomes 0 on the way to LDS, since 0 times what lies there need not be.
+        struct Loaded { H8 k[kLoads], v[kLoads]; uint32_t there; };     // of a unit; there: whose 16 keys lie in a page that is there, a bit to each
+        const int64_t row_bytes = a.cache.token_stride * 2;
+        auto group_of = [&](int l) { return uniform((l * kRowsOfLoad + wave * (64 / kChunks)) / 16); };      // the 16 keys that the wavefront's rows of a load are among
         auto fetch = [&](int u, Loaded &to) {
+            const int key0 = u * kWideKeys, in_page = (1 << shift) - 1;
+            if (key0 < p.see) pages.go(key0 >> shift);  // (16 keys lie in one page, and the unit's pages among 64 of the list's)
             to.there = 0;
-            int number[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {               // 16 keys lie in one page
-                const int key = u * kWideKeys + j * 16;
-                number[j] = pages.number(key >> shift);
-                to.there |= number[j] >= 0 && number[j] < a.cache.n_pages && key < p.see ? 0xffffull << (16 * j) : 0;
-            }
-            const bool whole = to.there == ~0ull && (u + 1) * kWideKeys <= p.see;
+            for (int j = 0; j < 4; ++j)
+                to.there |= (uint32_t)((pages.there >> (((key0 + j * 16) >> shift) & 63)) & 1) << j & (key0 + j * 16 < p.see ? 15u : 0u);
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
-                const int j = uniform((l * kRowsOfLoad + wave * (64 / kChunks)) / 16), key = u * kWideKeys + j * 16;      // the wavefront's rows of this load
-                const int which = uniform(j == 0 ? number[0] : j == 1 ? number[1] : j == 2 ? number[2] : number[3]);
-                const int64_t at = uniform(((int64_t)which * a.cache.page_stride + (int64_t)(key & ((1 << shift) - 1)) * a.cache.token_stride +
-                                            (int64_t)p.head * a.cache.head_stride) * 2);
-                const bool seen = whole || (((to.there >> (16 * j)) & 1) && key + (l_row & 15) < p.see);
-                if (!whole) { to.k[l] = zero; to.v[l] = zero; }
-                if (seen) {
-                    to.k[l] = *(const H8 *)((const char *)a.cache.k + at + l_at);
-                    to.v[l] = *(const H8 *)((const char *)a.cache.v + at + l_at);
-                }
+                const int j = group_of(l), key = key0 + j * 16;
+                const int64_t at = (to.there >> j) & 1 ? pages.at(key >> shift) + (uint32_t)(key & in_page) * (uint64_t)row_bytes : 0;
+                to.k[l] = *(const H8 *)((const char *)a.cache.k + at + l_at);
+                to.v[l] = *(const H8 *)((const char *)a.cache.v + at + l_at);
             }
         };
         const LdsBytes kv = lds_bytes(lds);
         const int k_to = k_at<D>(l_row, l_chunk), v_to = v_at<D>(l_row, l_chunk) + kTile;
-        auto store = [&](int buffer, const Loaded &from) {
+        auto store = [&](int buffer, Loaded &from, int u) {
             const LdsBytes k = kv + buffer * 2 * kTile;
+            if (from.there != 15 || (u + 1) * kWideKeys > p.see) {
+                asm volatile("");
+#pragma unroll
+                for (int l = 0; l < kLoads; ++l) {
+                    const int j = group_of(l);
+                    if (!((from.there >> j) & 1) || u * kWideKeys + j * 16 + (l_row & 15) >= p.see) from.v[l] = zero;
+                }
+            }
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {          // (the rows of a load differ from the first's in no bit that the layout looks at)
                 write_row<T>(k + k_to + l * kRowsOfLoad * D * 2, from.k[l]);
@@ -698,9 +733,9 @@ struct Wide {
         // is not to be seen by some row.
         const int s16 = lane & 15, k_lane = k_at<D>(lane & 31, half),
                   v_lane = v_at<D>(half * 4 + (s16 >> 2), ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8 + kTile;
-        auto attend = [&](const LdsBytes k, int key0, uint64_t there) {
+        auto attend = [&](const LdsBytes k, int key0, uint32_t there) {
             if (!busy || key0 > most) return;
-            const bool edge = key0 + kWideKeys - 1 > least || there != ~0ull;
+            const bool edge = key0 + kWideKeys - 1 > least || there != 15;
             f32x16 x[2];
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.0f;
@@ -719,11 +754,10 @@ struct Wide {
             if (edge) {
                 asm volatile("");                       // (a branch: few units have one)
                 const int last = position - key0 - half * 4;        // of the row's keys of this unit, counted from the lane's first
-                const uint64_t seen = there >> (half * 4);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     const int c = (i >> 4) * 32 + ((i & 15) >> 2) * 8 + (i & 3);
-                    if (c > last || !((seen >> c) & 1)) x[i >> 4][i & 15] = -__builtin_inff();
+                    if (c > last || !((there >> (c >> 4)) & 1)) x[i >> 4][i & 15] = -__builtin_inff();
                 }
             }
             float big = x[0][0];
@@ -767,22 +801,22 @@ struct Wide {
         Loaded odd, even;
         int u = p.unit0;
         fetch(u, even);
-        if (u + 1 < p.unit1) fetch(u + 1, odd);
-        store(0, even);
-        uint64_t there = even.there;
+        fetch(u + 1, odd);
+        store(0, even, u);
+        uint32_t there = even.there;
         __syncthreads();
         for (;;) {
-            if (u + 2 < p.unit1) fetch(u + 2, even);
+            fetch(u + 2, even);
             attend(kv, u * kWideKeys, there);
             if (u + 1 == p.unit1) break;
-            store(1, odd);
+            store(1, odd, u + 1);
             there = odd.there;
             __syncthreads();
             ++u;
-            if (u + 2 < p.unit1) fetch(u + 2, odd);
+            fetch(u + 2, odd);
             attend(kv + 2 * kTile, u * kWideKeys, there);
             if (u + 1 == p.unit1) break;
-            store(0, even);
+            store(0, even, u + 1);
             there = even.there;
             __syncthreads();
             ++u;
