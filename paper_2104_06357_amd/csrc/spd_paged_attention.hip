@@ -639,7 +639,12 @@ __global__ void __launch_bounds__(64) spd_paged_selected_join_kernel(const Paged
 
 // ---- many rows: a workgroup to 256 of them -------------------------------------------------------
 
-constexpr int kWideRows = 256, kWideKeys = 64, kWideWaves = 8;
+template <int D> struct WideShape;
+template <> struct WideShape<128> { static constexpr int kWaves = 8, kKeys = 64, kPerUnit = 2; };
+template <> struct WideShape<64> { static constexpr int kWaves = 4, kKeys = 64, kPerUnit = 3; };
+constexpr int wide_rows(int dim) { return 32 * (dim == 64 ? WideShape<64>::kWaves : WideShape<128>::kWaves); }
+constexpr int wide_keys(int dim) { return dim == 64 ? WideShape<64>::kKeys : WideShape<128>::kKeys; }
+constexpr int wide_groups(int dim) { return dim == 64 ? WideShape<64>::kPerUnit * 4 / WideShape<64>::kWaves : WideShape<128>::kPerUnit * 4 / WideShape<128>::kWaves; }
 
 struct WidePart {
     int request, first_token, position0, row0, rows, head;
@@ -651,10 +656,12 @@ template <spd_dtype T, int D>
 struct Wide {
     using H = half_t<T>;
     using H8 = half8_t<T>;
+    static constexpr int kWideWaves = WideShape<D>::kWaves, kWideKeys = WideShape<D>::kKeys, kWideRows = 32 * kWideWaves;
     static constexpr int kChunks = D / 8, kSteps = D / 16, kDims = D / 32;
     static constexpr int kThreads = kWideWaves * 64, kRowsOfLoad = kThreads / kChunks, kLoads = kWideKeys / kRowsOfLoad;
     static constexpr int kTile = kWideKeys * D * 2;     // bytes of K or V in LDS
     static constexpr int kAhead = 4;                    // reads of LDS that are on their way
+    static constexpr uint32_t kAllThere = (1u << (kWideKeys / 16)) - 1;
 
     H8 q[kSteps];
     f32x16 o[kDims];
@@ -701,8 +708,8 @@ struct Wide {
             if (key0 < p.see) pages.go(key0 >> shift);  // (16 keys lie in one page, and the unit's pages among 64 of the list's)
             to.there = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                to.there |= (uint32_t)((pages.there >> (((key0 + j * 16) >> shift) & 63)) & 1) << j & (key0 + j * 16 < p.see ? 15u : 0u);
+            for (int j = 0; j < kWideKeys / 16; ++j)
+                to.there |= (uint32_t)((pages.there >> (((key0 + j * 16) >> shift) & 63)) & 1) << j & (key0 + j * 16 < p.see ? kAllThere : 0u);
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
                 const int j = group_of(l), key = key0 + j * 16;
@@ -715,7 +722,7 @@ struct Wide {
         const int k_to = k_at<D>(l_row, l_chunk), v_to = v_at<D>(l_row, l_chunk) + kTile;
         auto store = [&](int buffer, Loaded &from, int u) {
             const LdsBytes k = kv + buffer * 2 * kTile;
-            if (from.there != 15 || (u + 1) * kWideKeys > p.see) {
+            if (from.there != kAllThere || (u + 1) * kWideKeys > p.see) {
                 asm volatile("");
 #pragma unroll
                 for (int l = 0; l < kLoads; ++l) {
@@ -729,13 +736,13 @@ struct Wide {
                 write_row<T>(k + v_to + l * kRowsOfLoad * D * 2, from.v[l]);
             }
         };
-        // K Q^T, a column to a lane: keys 32 t + 8 (i / 4) + 4 half + i % 4; then the softmax's weights, and V^T times them.  `edge`: some key
+        // 64 keys: K Q^T, a column to a lane: keys 32 t + 8 (i / 4) + 4 half + i % 4; then the softmax's weights, and V^T times them.  `edge`: some key
         // is not to be seen by some row.
         const int s16 = lane & 15, k_lane = k_at<D>(lane & 31, half),
                   v_lane = v_at<D>(half * 4 + (s16 >> 2), ((lane >> 4) & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8 + kTile;
         auto attend = [&](const LdsBytes k, int key0, uint32_t there) {
             if (!busy || key0 > most) return;
-            const bool edge = key0 + kWideKeys - 1 > least || there != 15;
+            const bool edge = key0 + 63 > least || there != 15;
             f32x16 x[2];
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.0f;
@@ -797,29 +804,24 @@ struct Wide {
             }
             __builtin_amdgcn_sched_barrier(0);
         };
-        // Unit u is in LDS while u + 1 and u + 2 are on their way in registers: memory has the time of two units to answer.
-        Loaded odd, even;
-        int u = p.unit0;
-        fetch(u, even);
-        fetch(u + 1, odd);
-        store(0, even, u);
-        uint32_t there = even.there;
+        // Unit u is in LDS while u + 1 is on its way in registers.
+        Loaded next;
+        int u = p.unit0, buffer = 0;
+        fetch(u, next);
+        store(0, next, u);
+        uint32_t there = next.there;
         __syncthreads();
         for (;;) {
-            fetch(u + 2, even);
-            attend(kv, u * kWideKeys, there);
+            const LdsBytes k = kv + buffer * 2 * kTile;
+            fetch(u + 1, next);
+#pragma unroll
+            for (int i = 0; i < kWideKeys / 64; ++i) attend(k + i * 128 * D, u * kWideKeys + i * 64, (there >> (4 * i)) & 15);
             if (u + 1 == p.unit1) break;
-            store(1, odd, u + 1);
-            there = odd.there;
-            __syncthreads();
+            buffer ^= 1;
             ++u;
-            fetch(u + 2, odd);
-            attend(kv + 2 * kTile, u * kWideKeys, there);
-            if (u + 1 == p.unit1) break;
-            store(0, even, u + 1);
-            there = even.there;
+            store(buffer, next, u);
+            there = next.there;
             __syncthreads();
-            ++u;
         }
         __syncthreads();                                // (the next segment's first unit goes where this one's last may be)
         sum = sum_of_2(sum);
@@ -880,15 +882,15 @@ __device__ __forceinline__ WidePart wide_part(const PagedAttention &a, const Til
     p.request = uniform(t.request);
     p.first_token = uniform(rq.first); p.position0 = uniform(rq.kv - rq.count);
     p.row0 = uniform(t.row0);
-    p.rows = uniform(min(kWideRows, rq.count * a.q.group - t.row0));
+    p.rows = uniform(min(wide_rows(a.head_dim), rq.count * a.q.group - t.row0));
     p.head = uniform(head);
     p.see = max(0, p.position0 + (p.row0 + p.rows - 1) / a.q.group + 1);
     return p;
 }
 
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kWideWaves * 64, 2) spd_paged_wide_kernel(const PagedAttention a, const Schedule s) {
-    __shared__ __align__(16) half_t<T> s_kv[4 * kWideKeys * D];
+__global__ void __launch_bounds__(WideShape<D>::kWaves * 64, WideShape<D>::kPerUnit) spd_paged_wide_kernel(const PagedAttention a, const Schedule s) {
+    __shared__ __align__(16) half_t<T> s_kv[4 * WideShape<D>::kKeys * D];         // two units of K and V
     const int n_tiles = s.n_tiles[0];
     const int64_t w = (int64_t)(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
     const int64_t per_head = n_tiles ? s.first[n_tiles] : 0, all = per_head * a.cache.kv_heads, workers = workers_for(all, (int64_t)gridDim.x, kWideLeast);
@@ -919,7 +921,7 @@ __global__ void __launch_bounds__(kWideWaves * 64, 2) spd_paged_wide_kernel(cons
 
 // A workgroup to a worker, as for few rows.
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kWideWaves * 64) spd_paged_wide_join_kernel(const PagedAttention a, const Schedule s) {
+__global__ void __launch_bounds__(WideShape<D>::kWaves * 64) spd_paged_wide_join_kernel(const PagedAttention a, const Schedule s) {
     const Joined j = s.joined[blockIdx.x];
     if (j.parts == 0) return;
     const int64_t w = blockIdx.x;
@@ -963,11 +965,11 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
     // A wavefront of the narrow kernel counts the units itself, 64 requests at a time and in 32 bits.
     const double most_units = (double)(rows / kNarrowRows + a.req.n_requests) * (double)((((int64_t)a.req.max_pages << a.cache.page_shift) + kNarrowKeys - 1) / kNarrowKeys + 1);
     c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256 || most_units * a.cache.kv_heads >= 2147483648.0;
-    c.rows = c.wide ? kWideRows : kNarrowRows;
-    c.keys = c.wide ? kWideKeys : kNarrowKeys;
-    c.threads = c.wide ? kWideWaves * 64 : 64;
+    c.rows = c.wide ? wide_rows(a.head_dim) : kNarrowRows;
+    c.keys = c.wide ? wide_keys(a.head_dim) : kNarrowKeys;
+    c.threads = c.wide ? 2 * c.rows : 64;
     const int groups = std::max(n_cus / 8, 1) * 8;          // as many to every XCD
-    c.workers = c.wide ? groups : groups * 2 * kNarrowWaves;
+    c.workers = c.wide ? groups * wide_groups(a.head_dim) : groups * 2 * kNarrowWaves;
     c.tiles = rows / c.rows + a.req.n_requests;
     return c;
 }
@@ -1010,8 +1012,8 @@ hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Sc
     }
     if (c.wide) {
         hipLaunchKernelGGL(spd_paged_schedule_kernel, dim3(1), dim3(kScheduleThreads), 0, st, a.req, a.cache.page_shift, a.q.group, c.rows, c.keys, s);
-        hipLaunchKernelGGL((spd_paged_wide_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s);
-        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kWideWaves * 64), 0, st, a, s);
+        hipLaunchKernelGGL((spd_paged_wide_kernel<T, D>), dim3((unsigned)c.workers), dim3(WideShape<D>::kWaves * 64), 0, st, a, s);
+        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(WideShape<D>::kWaves * 64), 0, st, a, s);
     } else {
         hipLaunchKernelGGL((spd_paged_narrow_kernel<T, D>), dim3((unsigned)(c.workers / kNarrowWaves)), dim3(kNarrowWaves * 64), 0, st, a, s);
         hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kNarrowWaves * 64), 0, st, a, s);
