@@ -39,8 +39,9 @@ constexpr int kScheduleThreads = 1024;
 // One workgroup: a wavefront to a request counts its tiles and units, a scan over the requests, and the tiles are written.
 __global__ void __launch_bounds__(kScheduleThreads) spd_paged_schedule_kernel(const PagedRequests req, const int shift, const int group,
                                                                                const int rows, const int keys, const Schedule s) {
-    __shared__ int64_t s_wave[kScheduleThreads / 64][2];
+    __shared__ int64_t s_wave[kScheduleThreads / 64][2], s_requests[2][kScheduleThreads];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, n = req.n_requests;
+    int64_t *const request_tiles = n <= kScheduleThreads ? s_requests[0] : s.request_tiles, *const request_units = n <= kScheduleThreads ? s_requests[1] : s.request_units;
     for (int r = wave; r < n; r += kScheduleThreads / 64) {
         const PagedRequest rq = paged_request(req, shift, r);
         const int tiles = (rq.count * group + rows - 1) / rows;
@@ -48,14 +49,14 @@ __global__ void __launch_bounds__(kScheduleThreads) spd_paged_schedule_kernel(co
         for (int i = lane; i < tiles; i += 64) units += tile_units(rq, group, rows, keys, i);
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) units += __shfl_xor(units, d);
-        if (lane == 0) { s.request_tiles[r] = tiles; s.request_units[r] = units; }
+        if (lane == 0) { request_tiles[r] = tiles; request_units[r] = units; }
     }
     __threadfence_block();
     __syncthreads();
     int64_t tiles = 0, units = 0;
     for (int base = 0; base < n; base += kScheduleThreads) {
         const int r = base + tid;
-        const int64_t a = r < n ? s.request_tiles[r] : 0, b = r < n ? s.request_units[r] : 0;
+        const int64_t a = r < n ? request_tiles[r] : 0, b = r < n ? request_units[r] : 0;
         int64_t ia = a, ib = b;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(kScheduleThreads) spd_paged_schedule_kernel(co
             if (w < wave) { ia += s_wave[w][0]; ib += s_wave[w][1]; }
             ta += s_wave[w][0]; tb += s_wave[w][1];
         }
-        if (r < n) { s.request_tiles[r] = tiles + ia - a; s.request_units[r] = units + ib - b; }
+        if (r < n) { request_tiles[r] = tiles + ia - a; request_units[r] = units + ib - b; }
         tiles += ta; units += tb;
         __syncthreads();
     }
@@ -83,8 +84,8 @@ __global__ void __launch_bounds__(kScheduleThreads) spd_paged_schedule_kernel(co
     for (int r = wave; r < n; r += kScheduleThreads / 64) {
         const PagedRequest rq = paged_request(req, shift, r);
         const int many = (rq.count * group + rows - 1) / rows;
-        int64_t before = s.request_units[r];
-        const int64_t at = s.request_tiles[r];
+        int64_t before = request_units[r];
+        const int64_t at = request_tiles[r];
         for (int i0 = 0; i0 < many; i0 += 64) {
             const int i = i0 + lane, u = i < many ? tile_units(rq, group, rows, keys, i) : 0;
             int sum = u;
@@ -854,24 +855,6 @@ struct Wide {
             for (int i = 0; i < 4; ++i) to[(d * 4 + i) * kThreads + tid] = f32x4{o[d][i * 4], o[d][i * 4 + 1], o[d][i * 4 + 2], o[d][i * 4 + 3]};
         s.stats[slot * kThreads + tid] = make_float2(top, sum);
     }
-
-    __device__ __forceinline__ void join(const Schedule &s, int64_t slot) {
-        const int tid = (int)threadIdx.x;
-        const float2 st = s.stats[slot * kThreads + tid];
-        const f32x4 *const from = (const f32x4 *)(s.sums + slot * (kWideRows * D));
-        const float to = fmaxf(top, st.x), mine = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(top - to),
-                    theirs = to == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(st.x - to);
-        top = to;
-        sum = sum * mine + st.y * theirs;
-#pragma unroll
-        for (int d = 0; d < kDims; ++d)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 x = from[(d * 4 + i) * kThreads + tid];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[d][i * 4 + e] = o[d][i * 4 + e] * mine + x[e] * theirs;
-            }
-    }
 };
 
 constexpr int64_t kWideLeast = 2;
@@ -909,7 +892,7 @@ __global__ void __launch_bounds__(WideShape<D>::kWaves * 64, WideShape<D>::kPerU
         if (p.unit0 == 0 && p.unit1 == t.units) n.write(a, p);
         else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
         if (p.unit0 == 0 && p.unit1 < t.units)
-            joined = Joined{(int)(worker_of(all, workers, place.segment_begin + t.units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, 0};
+            joined = Joined{(int)(worker_of(all, workers, place.segment_begin + t.units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, (int)w};
         at = place.segment_begin + p.unit1;
         if (p.unit1 == t.units) {
             place.segment_begin = at;
@@ -919,19 +902,51 @@ __global__ void __launch_bounds__(WideShape<D>::kWaves * 64, WideShape<D>::kPerU
     if (threadIdx.x == 0) s.joined[w] = joined;
 }
 
-// A workgroup to a worker, as for few rows.
+// A workgroup to a worker, as for few rows, and to 32 of the places.
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(WideShape<D>::kWaves * 64) spd_paged_wide_join_kernel(const PagedAttention a, const Schedule s) {
+    using H = half_t<T>;
+    constexpr int kThreads = WideShape<D>::kWaves * 64, kRows = wide_rows(D);
     const Joined j = s.joined[blockIdx.x];
     if (j.parts == 0) return;
-    const int64_t w = blockIdx.x;
-    Wide<T, D> n;
-    n.clear();
-    n.join(s, 2 * w + 1);
-    for (int i = 1; i < j.parts; ++i) n.join(s, 2 * (w + i));
-    WidePart p{};
-    p.first_token = j.first_token; p.row0 = j.row0; p.rows = j.rows; p.head = j.head;
-    n.write(a, p);
+    const int64_t w = j.worker;
+    const int tid = (int)threadIdx.x, lane = tid & 63, half = lane >> 5, mine = (tid >> 6) * 32 + (lane & 31), d = (int)blockIdx.y;
+    f32x4 o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = f32x4{0, 0, 0, 0};
+    float top = -__builtin_inff(), sum = 0.0f;
+    for (int part = 0; part < j.parts; part += 2) {     // two on their way
+        const bool second = part + 1 < j.parts;
+        const int64_t slots[2] = {part == 0 ? 2 * w + 1 : 2 * (w + part), second ? 2 * (w + part + 1) : 2 * w + 1};
+        float2 st[2];
+        f32x4 x[2][4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const f32x4 *const from = (const f32x4 *)(s.sums + slots[b] * (kRows * D));
+            st[b] = s.stats[slots[b] * kThreads + tid];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[b][i] = from[(d * 4 + i) * kThreads + tid];
+        }
+        if (!second) st[1] = make_float2(-__builtin_inff(), 0.0f);
+        const float to = fmaxf(top, fmaxf(st[0].x, st[1].x)), base = to == -__builtin_inff() ? 0.0f : to;
+        const float kept = __builtin_amdgcn_exp2f(top - base), e0 = __builtin_amdgcn_exp2f(st[0].x - base), e1 = __builtin_amdgcn_exp2f(st[1].x - base);
+        top = to;
+        sum = sum * kept + (st[0].y * e0 + st[1].y * e1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = o[i] * kept + (x[0][i] * e0 + x[1][i] * e1);
+    }
+    if (mine >= j.rows) return;
+    const int f = j.row0 + mine, token = f / a.q.group, g = f - token * a.q.group;
+    const int64_t at = (int64_t)(j.first_token + token) * a.q.heads + (int64_t)j.head * a.q.group + g;
+    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        half4_t<T> r;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = (H)(o[i][e] * by);
+        *(half4_t<T> *)((H *)a.out.out + at * D + d * 32 + i * 8 + half * 4) = r;
+    }
+    if (d == 0 && half == 0 && a.out.lse) a.out.lse[at] = sum > 0.0f ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : -__builtin_inff();
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -1013,7 +1028,7 @@ hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Sc
     if (c.wide) {
         hipLaunchKernelGGL(spd_paged_schedule_kernel, dim3(1), dim3(kScheduleThreads), 0, st, a.req, a.cache.page_shift, a.q.group, c.rows, c.keys, s);
         hipLaunchKernelGGL((spd_paged_wide_kernel<T, D>), dim3((unsigned)c.workers), dim3(WideShape<D>::kWaves * 64), 0, st, a, s);
-        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(WideShape<D>::kWaves * 64), 0, st, a, s);
+        hipLaunchKernelGGL((spd_paged_wide_join_kernel<T, D>), dim3((unsigned)c.workers, D / 32), dim3(WideShape<D>::kWaves * 64), 0, st, a, s);
     } else {
         hipLaunchKernelGGL((spd_paged_narrow_kernel<T, D>), dim3((unsigned)(c.workers / kNarrowWaves)), dim3(kNarrowWaves * 64), 0, st, a, s);
         hipLaunchKernelGGL((spd_paged_narrow_join_kernel<T, D>), dim3((unsigned)c.workers), dim3(kNarrowWaves * 64), 0, st, a, s);

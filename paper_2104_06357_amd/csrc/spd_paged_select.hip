@@ -18,7 +18,7 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     if (x != x) return 1;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-constexpr uint32_t kForced = 0xffffffffu, kAbsent = 2;
+constexpr uint32_t kForced = 0xffffffffu, kAbsent = 2;            // (no score has the first: it would be no number)
 
 // A wavefront chooses the `k` greatest of `n` keys, equal ones by the lower number, and hands each to `take(rank, number)`, rank
 // ascending with the number.  Lane l holds the numbers l * each .. + each - 1, each <= kSelectEach.  The k-th key is found bit by bit: the keys at
@@ -32,10 +32,28 @@ __device__ __forceinline__ void choose_of(int n, int k, int each, Key key, Take 
         mine[j] = 0;
         if (j < each && first + j < n) mine[j] = key(first + j);
     }
-    uint32_t floor = 0;
+    // Those that are forced come first; the others' first bits are mostly the same, and the search begins behind them.
+    uint32_t most = 0, least = ~0u;
+    int forced = 0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const bool is = mine[j] == kForced;
+        forced += __popcll(__ballot(is));
+        most = max(most, is ? 0u : mine[j]);
+        least = min(least, mine[j] == 0 ? ~0u : mine[j]);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) { most = max(most, (uint32_t)__shfl_xor((int)most, d)); least = min(least, (uint32_t)__shfl_xor((int)least, d)); }
+    most = (uint32_t)uniform((int)most); least = (uint32_t)uniform((int)least);
+    uint32_t floor = kForced;
+    int bit = -1;
+    if (k > forced) {
+        bit = most == least ? -1 : 31 - __builtin_clz(most ^ least);
+        floor = bit < 0 ? most : most & ~((2u << bit) - 1);
+    }
     bool exact = false;                                           // as many as k lie at or above `floor`
 #pragma unroll 1
-    for (int bit = 31; bit >= 0 && !exact; --bit) {
+    for (; bit >= 0 && !exact; --bit) {
         const uint32_t to = floor | 1u << bit;
         int count = 0;
 #pragma unroll
@@ -108,23 +126,34 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
     if (most > a.n_select) {
         const int low = lane & 15, quad = lane >> 4;
         const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride + page0;
-        i32x4 c[kSteps];
-        float scale;
-        auto fetch = [&](int p0) {
-            const int32_t number = p0 + low < pages ? table[p0 + low] : -1;
+        // A wavefront's page numbers, 4 steps' to a load, then the codes of two steps, on their way while the queries are.
+        constexpr int kStride = kSelectTokens * 16, kRounds = kSelectPages / kStride / 4;
+        int32_t numbers[kRounds];
+#pragma unroll
+        for (int i = 0; i < kRounds; ++i) {
+            const int p = wave * 16 + (i * 4 + quad) * kStride + low;
+            numbers[i] = p < pages ? table[p] : -1;
+        }
+        struct Codes { i32x4 c[kSteps]; float scale; } codes[2];
+        auto fetch = [&](int step, Codes &to) {
+            int number = -1;
+#pragma unroll
+            for (int i = 0; i < kRounds; ++i) if (step >> 2 == i) number = __shfl(numbers[i], (step & 3) * 16 + low);
             const bool there = number >= 0 && number < a.cache.n_pages;
             const int64_t at = (int64_t)(there ? number : 0) * a.cache.kv_heads + kvh;
-            scale = -__builtin_inff();                            // (marks a page that is not there)
+            to.scale = -__builtin_inff();                         // (marks a page that is not there)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) c[s] = i32x4{0, 0, 0, 0};
+            for (int s = 0; s < kSteps; ++s) to.c[s] = i32x4{0, 0, 0, 0};
             if (there) {
                 const int8_t *const from = a.cache.codes + at * 2 * D + quad * 16;
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) c[s] = *(const i32x4 *)(from + s * 64);
-                scale = a.cache.code_scale[at];
+                for (int s = 0; s < kSteps; ++s) to.c[s] = *(const i32x4 *)(from + s * 64);
+                to.scale = a.cache.code_scale[at];
             }
         };
-        if (wave * 16 < pages) fetch(wave * 16);                  // (on its way while the queries are)
+        const int steps = pages > wave * 16 ? (pages - wave * 16 + kStride - 1) / kStride : 0;
+        if (steps > 0) fetch(0, codes[0]);
+        if (steps > 1) fetch(1, codes[1]);
         if (wave < tile.count) {
             const H *const q = (const H *)a.q.ptr + (int64_t)(tile.first + wave) * a.q.token_stride + (int64_t)kvh * group * a.q.head_stride + lane * E;
             constexpr int kHeld = 8;                              // heads that stay in registers between the two passes
@@ -132,7 +161,7 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
 #pragma unroll
             for (int g = 0; g < kHeld; ++g)
 #pragma unroll
-                for (int e = 0; e < E; ++e) held[g][e] = g < group ? (float)q[g * a.q.head_stride + e] : 0.0f;
+                for (int e = 0; e < E; ++e) held[g][e] = (float)q[min(g, group - 1) * a.q.head_stride + e];
 #pragma unroll
             for (int g = 0; g < kHeld; ++g)
 #pragma unroll
@@ -172,22 +201,27 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = *(const i32x4 *)&s_code[low][s * 64 + quad * 16];
         const int own = low < tile.count && position0 + low >= 0 ? (position0 + low) >> shift : -1;    // of token `low`
-        for (int p0 = wave * 16; p0 < pages; p0 += kSelectTokens * 16) {
+        auto score = [&](int step, Codes &of) {
+            const int p0 = wave * 16 + step * kStride;
             i32x4 x = {0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_i32_16x16x64_i8(c[s], q[s], x, 0, 0, 0);
-            const float scale_now = scale;
-            if (p0 + kSelectTokens * 16 < pages) fetch(p0 + kSelectTokens * 16);
+            for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_i32_16x16x64_i8(of.c[s], q[s], x, 0, 0, 0);
+            const float scale = of.scale;
+            if (step + 2 < steps) fetch(step + 2, of);
             uint32_t key[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float of_page = __shfl(scale_now, quad * 4 + i);
+                const float of_page = __shfl(scale, quad * 4 + i);
                 const int p = page0 + p0 + quad * 4 + i;
                 key[i] = of_page == -__builtin_inff() ? kAbsent : key_of((float)x[i] * of_page);
                 if (p == 0 || p == own) key[i] = kForced;
                 if (p > own) key[i] = 0;
             }
             *(uint4 *)&s_key[low * room + p0 + quad * 4] = make_uint4(key[0], key[1], key[2], key[3]);
+        };
+        for (int step = 0; step < steps; step += 2) {
+            score(step, codes[0]);
+            if (step + 1 < steps) score(step + 1, codes[1]);
         }
         __syncthreads();
     }
