@@ -227,6 +227,42 @@ def test_attention_types_and_layouts(spd, h, shape, dtype, dim, layout, page):
     assert_close(w, run_chunk(spd, h, w, scale=0.2), w.attention(scale=0.2), shape)
 
 
+# requests are counted 64 at a time, by a wavefront up to 256 of them, in LDS up to 1,024
+@pytest.mark.parametrize("n", [64, 65, 200, 256, 257, 1025])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_of_many_requests(spd, h, n, dim):
+    rng = np.random.default_rng(n)
+    requests = [(int(rng.integers(0, 90)), int(rng.choice([0, 1, 1, 1, 2]))) for _ in range(n)]
+    requests[0], requests[-1] = (40, 0), (700, 1)
+    w = World(requests, dim=dim, kv_heads=1, group=2, seed=n)
+    print("attention of", n, "requests", flush=True)
+    assert_close(w, run_chunk(spd, h, w), w.attention(), "%d requests" % n)
+    w.make_bounds()
+    check_sparse(spd, h, w, 3, "%d requests" % n)
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "f16"), (128, "bf16")])
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+def test_attention_of_long_chunks(spd, h, page, dim, dtype):
+    """Several tiles of rows and units of keys, cut among the workgroups inside segments; pages that are missing in the middle."""
+    w = World([(900, 150), (3, 260), (130, 1)], page=page, dim=dim, dtype=dtype, kv_heads=2, group=4, layout="htd", seed=page + dim)
+    if page <= 64:
+        w.table[0, 3], w.table[0, 9 if page < 64 else 5], w.table[1, 1] = -1, w.pages, -7
+    print("long chunks", page, dim, flush=True)
+    assert_close(w, run_chunk(spd, h, w), w.attention(), "long chunks")
+
+
+def test_attention_over_an_empty_cache(spd, h):
+    """No pages at all: nobody sees anything."""
+    for tokens in (1, 90):
+        k = torch.zeros((0, 16, 2, 64), dtype=torch.bfloat16, device="cuda")
+        cache = spd.PagedCache(k, k.clone())
+        batch = spd.PagedBatch(torch.tensor([0, tokens], dtype=torch.int32, device="cuda"), torch.tensor([200], dtype=torch.int32, device="cuda"),
+                               torch.full((1, 20), 3, dtype=torch.int32, device="cuda"))
+        out, lse = h.paged_attention(cache, torch.randn((tokens, 4, 64), device="cuda").to(torch.bfloat16), batch)
+        assert not bool(out.any()) and bool(torch.isinf(lse).all())
+
+
 def test_attention_rows_that_see_nothing(spd, h):
     """Fewer cached tokens than new ones: the first rows stand before the request begins.  Pages that are not there mask theirs; a length
     past the table is cut; tokens outside every request are left alone."""
@@ -256,6 +292,17 @@ def test_attention_lengths_that_contradict_the_arrays(spd, h):
     for starts, lens in (([0, 4, 100], [34, 16]), ([0, 8, 3], [34, 16]), ([-5, 4, 10], [34, 16]), ([0, 4, 10], [-3, 16])):
         w.query_start, w.kv_lens = torch.tensor(starts, dtype=torch.int32), torch.tensor(lens, dtype=torch.int32)
         out, lse = run_chunk(spd, h, w)
+        torch.cuda.synchronize()
+    # requests that overlap, as many as can be, of both kernels and of the selection
+    for n, tokens in ((40, 30), (100, 30), (300, 30), (40, 400), (1100, 50)):
+        o = World([(50, 1)] * n, group=4, kv_heads=1, dim=64, seed=n)
+        o.make_bounds()
+        o.query_start = torch.tensor([0, tokens] * (n // 2) + [0], dtype=torch.int32)
+        o.q = torch.zeros((tokens, 4, 64), dtype=torch.bfloat16)
+        o.tokens = tokens
+        print("overlapping", n, tokens, flush=True)
+        h.paged_attention(o.cache(spd), o.q.cuda(), o.batch(spd))
+        h.paged_sparse_attention(o.cache(spd), o.q.cuda(), o.batch(spd), 3)
         torch.cuda.synchronize()
     w.query_start, w.kv_lens = torch.tensor([0, 4, 10], dtype=torch.int32), torch.tensor([-3, 16], dtype=torch.int32)
     assert_close(w, run_chunk(spd, h, w), w.attention(), "a negative length")
@@ -348,6 +395,32 @@ def test_sparse_pages_that_are_not_there_and_queries_of_zero(spd, h):
     w.q[1] = 0
     w.kv_lens[2] = 12                                                       # 18 rows see nothing
     check_sparse(spd, h, w, 6, "missing pages")
+
+
+@pytest.mark.parametrize("pages,n_select", [(2047, 5), (2048, 64), (2049, 64), (2049, 2), (5000, 33), (67_700, 64)])
+def test_sparse_of_very_long_requests(spd, h, pages, n_select):
+    """More pages than a workgroup scores, and than lists of the best that a lane has room for."""
+    w = World([(16 * pages - 2, 3), (50, 1)], kv_heads=1, group=2, dim=64, seed=pages, drift=0.7)
+    print("sparse of", pages, "pages", flush=True)
+    check_sparse(spd, h, w, n_select, "%d pages" % pages)
+
+
+def test_sparse_of_a_table_wider_than_its_requests(spd, h):
+    w = World([(700, 2), (40, 17)], kv_heads=2, group=2, dim=64, seed=3, drift=0.7, wide=5000)
+    check_sparse(spd, h, w, 6, "wide table")
+
+
+@pytest.mark.parametrize("dim,page,n_select", [(128, 128, 64), (64, 1024, 9), (128, 256, 20)])
+def test_sparse_of_one_token_over_large_pages(spd, h, dim, page, n_select):
+    """A token's pages shared by several workgroups, whose sums are joined."""
+    w = World([(page * 100 + 17, 1), (page * 3, 1)], kv_heads=1, group=3, dim=dim, page=page, seed=page, drift=0.7)
+    check_sparse(spd, h, w, n_select, "large pages")
+
+
+def test_sparse_a_wavefront_to_a_segment(spd, h):
+    """Tokens and key heads enough for the chip."""
+    w = World([(400, 500), (30, 120)], kv_heads=4, group=3, dim=64, page=32, seed=13, drift=0.7)
+    check_sparse(spd, h, w, 7, "many segments")
 
 
 def test_sparse_of_many_tokens_and_a_wide_table(spd, h):
