@@ -174,32 +174,41 @@ class DeviceCsr:
                          self.host_indptr.ctypes.data if self.host_indptr is not None else None)
 
 
+_torch = None          # set with the first handle or cache: an import statement in a call that takes microseconds is a tenth of it
+
+
+def _need_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _rows(x, heads, cache, name):
     """A (tokens, heads, head_dim) tensor of the cache's type as spd_rows: any strides of tokens and heads."""
-    if x.dtype != cache.k.dtype or x.device != cache.k.device:
+    k = cache.k
+    if x.dtype is not k.dtype or x.device != k.device:
         raise ValueError("%s must have the cache's type and device" % name)
-    if x.dim() != 3 or x.shape[2] != cache.k.shape[3] or (heads and x.shape[1] != heads):
-        raise ValueError("%s must be (tokens, %s, %d)" % (name, heads or "heads", cache.k.shape[3]))
-    stride = x.stride()
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[2] != cache._dim or (heads and shape[1] != heads):
+        raise ValueError("%s must be (tokens, %s, %d)" % (name, heads or "heads", cache._dim))
     if stride[2] != 1 and x.numel():
         raise ValueError("the places of a head must lie next to each other in %s" % name)
     return RowsStruct(x.data_ptr(), stride[0], stride[1])
 
 
 def _out(x, shape, dtype, device, name):
-    import torch
     if x is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if x.dtype != dtype or x.device != device or tuple(x.shape) != shape or not x.is_contiguous():
+        return _need_torch().empty(shape, dtype=dtype, device=device)
+    if x.dtype is not dtype or x.shape != shape or x.device != device or not x.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of %s on %s" % (name, dtype, shape, device))
     return x
 
 
 def _int32(x, dims, device, name):
-    import torch
-    if x.dtype != torch.int32 or x.dim() != dims or x.device != device or (x.numel() and x.stride(-1) != 1):
+    if x.dtype is not _torch.int32 or x.device != device or x.dim() != dims or (x.stride(-1) != 1 and x.numel()):
         raise ValueError("%s must be a %d-dimensional int32 tensor on %s, its last dimension without gaps" % (name, dims, device))
-    return x
 
 
 class PagedCache:
@@ -209,7 +218,7 @@ class PagedCache:
     paged_sparse_attention selects pages by; bounds=True makes them, for a cache that is empty."""
 
     def __init__(self, k, v, bounds=None, codes=None, code_scale=None):
-        import torch
+        torch = _need_torch()
         dtypes = {torch.bfloat16: 0, torch.float16: 1}                       # spd_dtype
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in dtypes or k.device != v.device or not k.is_cuda:
             raise ValueError("k and v must be (pages, page_size, heads, head_dim) tensors of one 16-bit type on the GPU")
@@ -227,6 +236,7 @@ class PagedCache:
                                        (k.dtype, torch.int8, torch.float32)):
                 _out(x, shape, dtype, k.device, "bounds, codes or code_scale")
         self.k, self.v, self.bounds, self.codes, self.code_scale = k, v, bounds, codes, code_scale
+        self._heads, self._dim = heads, dim
         at = [x.data_ptr() if x is not None else None for x in kept]
         self._struct = PagedCacheStruct(dtypes[k.dtype], page, heads, dim, pages, k.data_ptr(), v.data_ptr(), k.stride(0),
                                         k.stride(1), k.stride(2), *at)
@@ -238,6 +248,7 @@ class PagedBatch:
     Handle.paged_plan also `slots` (int64), `positions` and `counts` of the new tokens."""
 
     def __init__(self, query_start, kv_lens, block_table):
+        _need_torch()
         _int32(query_start, 1, block_table.device, "query_start")
         _int32(kv_lens, 1, block_table.device, "kv_lens")
         _int32(block_table, 2, block_table.device, "block_table")
@@ -245,7 +256,7 @@ class PagedBatch:
         if not block_table.is_cuda or query_start.shape[0] != n + 1 or block_table.shape[0] != n:
             raise ValueError("query_start, kv_lens and block_table must be of n + 1, n and n requests, on the GPU")
         self.query_start, self.kv_lens, self.block_table = query_start, kv_lens, block_table
-        self.slots = self.positions = self.counts = None
+        self.slots = self.positions = self.counts = self._step = None
         self._struct = PagedBatchStruct(n, 0, block_table.shape[1], query_start.data_ptr(), kv_lens.data_ptr(),
                                         block_table.data_ptr(), block_table.stride(0))
         self._ref = ctypes.byref(self._struct)
@@ -258,6 +269,7 @@ class Handle:
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("spd needs a GPU: torch.cuda.is_available() is False")
+        _need_torch()
         self._lib = lib()
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         self._h = ctypes.c_void_p()
@@ -391,36 +403,37 @@ class Handle:
         """Block table (in place), slots and positions of a step's new tokens, from the requests' lengths, on the GPU
         (spd_paged_plan).  `n_tokens`: how many new tokens there are, or more; `out`: a PagedBatch of an earlier step with the same
         sizes, whose tensors are written again."""
-        import torch
+        torch = _need_torch()
         device, n = block_table.device, past_lens.shape[0]
-        for x, dims, name in ((past_lens, 1, "past_lens"), (new_lens, 1, "new_lens"), (free_pages, 1, "free_pages"),
-                              (block_table, 2, "block_table")):
-            _int32(x, dims, device, name)
-        if not block_table.is_cuda or new_lens.shape[0] != n or block_table.shape[0] != n:
-            raise ValueError("past_lens, new_lens and block_table must be of the same requests, on the GPU")
+        _int32(past_lens, 1, device, "past_lens")
+        _int32(new_lens, 1, device, "new_lens")
+        _int32(free_pages, 1, device, "free_pages")
         if out is None:
             i32 = {"dtype": torch.int32, "device": device}
             out = PagedBatch(torch.empty(n + 1, **i32), torch.empty(n, **i32), block_table)
             out.slots = torch.empty(n_tokens, dtype=torch.int64, device=device)
             out.positions, out.counts = torch.empty(n_tokens, **i32), torch.empty(3, **i32)
-        elif out.slots is None or out.slots.shape[0] != n_tokens or out.kv_lens.shape[0] != n or out.block_table is not block_table:
+            out._step = PagedStepStruct(n, n_tokens, block_table.shape[1], 0, 0, None, None, None, block_table.data_ptr(), block_table.stride(0),
+                                        out.query_start.data_ptr(), out.kv_lens.data_ptr(), out.slots.data_ptr(),
+                                        out.positions.data_ptr(), out.counts.data_ptr())
+        step = out._step
+        if step is None or step.n_tokens != n_tokens or step.n_requests != n or out.block_table is not block_table:
             raise ValueError("out must be a PagedBatch that paged_plan made for this block table and these sizes")
-        step = PagedStepStruct(n, n_tokens, block_table.shape[1], free_pages.shape[0], int(page_size), past_lens.data_ptr(),
-                               new_lens.data_ptr(), free_pages.data_ptr(), block_table.data_ptr(), block_table.stride(0),
-                               out.query_start.data_ptr(), out.kv_lens.data_ptr(), out.slots.data_ptr(),
-                               out.positions.data_ptr(), out.counts.data_ptr())
+        if new_lens.shape[0] != n:
+            raise ValueError("past_lens, new_lens and block_table must be of the same requests")
+        step.n_free, step.page_size, step.block_table = free_pages.shape[0], page_size, block_table.data_ptr()
+        step.past_lens, step.new_lens, step.free_pages = past_lens.data_ptr(), new_lens.data_ptr(), free_pages.data_ptr()
         self._check(self._lib.spd_paged_plan(self._h, ctypes.byref(step)))
         return out
 
     def paged_append(self, cache: PagedCache, k_new, v_new, slots):
         """Row t of `k_new` and `v_new` (tokens, heads, head_dim) into the cache's slot slots[t] (int64; -1 drops the row), and
         the bounds of the pages that get one (spd_paged_append)."""
-        import torch
-        heads, n = cache.k.shape[2], k_new.shape[0]
-        rows = [_rows(x, heads, cache, name) for x, name in ((k_new, "k_new"), (v_new, "v_new"))]
-        if v_new.shape[0] != n or slots.shape != (n,) or slots.dtype != torch.int64 or slots.device != k_new.device or not slots.is_contiguous():
+        heads, n = cache._heads, k_new.shape[0]
+        k_rows, v_rows = _rows(k_new, heads, cache, "k_new"), _rows(v_new, heads, cache, "v_new")
+        if v_new.shape[0] != n or slots.shape != (n,) or slots.dtype is not _torch.int64 or slots.device != k_new.device or not slots.is_contiguous():
             raise ValueError("slots must be int64, contiguous, on the cache's device, and as many as rows of k_new and of v_new")
-        self._check(self._lib.spd_paged_append(self._h, cache._ref, n, ctypes.byref(rows[0]), ctypes.byref(rows[1]), slots.data_ptr()))
+        self._check(self._lib.spd_paged_append(self._h, cache._ref, n, ctypes.byref(k_rows), ctypes.byref(v_rows), slots.data_ptr()))
 
     def paged_workspace_bytes(self, cache: PagedCache, batch: PagedBatch, n_tokens: int, n_heads: int, n_select: int = 0) -> int:
         """Scratch of one paged_attention, or with `n_select` paged_sparse_attention, call (spd_paged_workspace_bytes)."""
@@ -433,11 +446,10 @@ class Handle:
     def paged_attention(self, cache: PagedCache, q, batch: PagedBatch, scale=None, out=None, lse=None):
         """(out, lse): attention of the new tokens' queries `q` (tokens, heads, head_dim) over their requests' pages, each up to
         its own position (spd_paged_attention).  `scale` is 1/sqrt(head_dim) unless given."""
-        import torch
         t, heads, dim = q.shape
         rows, device = _rows(q, 0, cache, "q"), q.device
         out = _out(out, (t, heads, dim), q.dtype, device, "out")
-        lse = _out(lse, (t, heads), torch.float32, device, "lse")
+        lse = _out(lse, (t, heads), _torch.float32, device, "lse")
         batch._struct.n_tokens = t
         self._check(self._lib.spd_paged_attention(self._h, cache._ref, batch._ref, ctypes.byref(rows), heads,
                                                   dim ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr()))
@@ -447,12 +459,11 @@ class Handle:
         """(out, lse, selected): the same over `n_select` pages of each token and key head, the request's first, the token's own
         and those whose bounds score best; selected (tokens, key heads, n_select) are their places in the block table, ascending,
         then -1 (spd_paged_sparse_attention)."""
-        import torch
         t, heads, dim = q.shape
         rows, device = _rows(q, 0, cache, "q"), q.device
         out = _out(out, (t, heads, dim), q.dtype, device, "out")
-        lse = _out(lse, (t, heads), torch.float32, device, "lse")
-        selected = _out(selected, (t, cache.k.shape[2], max(int(n_select), 0)), torch.int32, device, "selected")
+        lse = _out(lse, (t, heads), _torch.float32, device, "lse")
+        selected = _out(selected, (t, cache._heads, max(int(n_select), 0)), _torch.int32, device, "selected")
         batch._struct.n_tokens = t
         self._check(self._lib.spd_paged_sparse_attention(self._h, cache._ref, batch._ref, ctypes.byref(rows), heads,
                                                          dim ** -0.5 if scale is None else scale, n_select, selected.data_ptr(),

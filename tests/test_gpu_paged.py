@@ -639,3 +639,17 @@ def test_profile_names_the_launches(spd):
     h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 4)
     assert [r["name"] for r in h.profile_read()] == ["paged_select", "paged_attention"]
     h.close()
+
+
+def test_the_example_answers_from_passages(capsys):
+    """Sparse k-NN, the passages' pages in the questions' block tables, and all four calls, as a program uses them."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "answer_from_passages.py")
+    spec = importlib.util.spec_from_file_location("answer_from_passages", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    hits, (off, log_off), finite = example.main()
+    assert hits == example.QUESTIONS and finite
+    # two ways of cutting the same sums: each rounds weights and result to bfloat16 (2^-8 of values below 6, twice), logits in fp32
+    assert off <= 4 * 2.0 ** -8 * 6 and log_off <= 3e-4
