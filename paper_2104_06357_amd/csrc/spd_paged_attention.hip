@@ -857,7 +857,7 @@ struct Wide {
     }
 };
 
-constexpr int64_t kWideLeast = 2;
+constexpr int64_t kWideLeast = 4;       // units of a worker at the least: each more part is more to join
 
 __device__ __forceinline__ WidePart wide_part(const PagedAttention &a, const Tile &t, int head) {
     const PagedRequest rq = paged_request(a.req, a.cache.page_shift, t.request);
@@ -915,25 +915,34 @@ __global__ void __launch_bounds__(WideShape<D>::kWaves * 64) spd_paged_wide_join
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] = f32x4{0, 0, 0, 0};
     float top = -__builtin_inff(), sum = 0.0f;
-    for (int part = 0; part < j.parts; part += 2) {     // two on their way
-        const bool second = part + 1 < j.parts;
-        const int64_t slots[2] = {part == 0 ? 2 * w + 1 : 2 * (w + part), second ? 2 * (w + part + 1) : 2 * w + 1};
-        float2 st[2];
-        f32x4 x[2][4];
+    constexpr int kFlight = 4;                          // parts that are on their way together
+    for (int part = 0; part < j.parts; part += kFlight) {
+        float2 st[kFlight];
+        f32x4 x[kFlight][4];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const f32x4 *const from = (const f32x4 *)(s.sums + slots[b] * (kRows * D));
-            st[b] = s.stats[slots[b] * kThreads + tid];
+        for (int b = 0; b < kFlight; ++b) {             // (past the last one the last one again, with no weight)
+            const int i = min(part + b, j.parts - 1);
+            const int64_t slot = i == 0 ? 2 * w + 1 : 2 * (w + i);
+            const f32x4 *const from = (const f32x4 *)(s.sums + slot * (kRows * D));
+            st[b] = s.stats[slot * kThreads + tid];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[b][i] = from[(d * 4 + i) * kThreads + tid];
+            for (int e = 0; e < 4; ++e) x[b][e] = from[(d * 4 + e) * kThreads + tid];
         }
-        if (!second) st[1] = make_float2(-__builtin_inff(), 0.0f);
-        const float to = fmaxf(top, fmaxf(st[0].x, st[1].x)), base = to == -__builtin_inff() ? 0.0f : to;
-        const float kept = __builtin_amdgcn_exp2f(top - base), e0 = __builtin_amdgcn_exp2f(st[0].x - base), e1 = __builtin_amdgcn_exp2f(st[1].x - base);
-        top = to;
-        sum = sum * kept + (st[0].y * e0 + st[1].y * e1);
+        float to = top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = o[i] * kept + (x[0][i] * e0 + x[1][i] * e1);
+        for (int b = 0; b < kFlight; ++b) to = fmaxf(to, st[b].x);
+        const float base = to == -__builtin_inff() ? 0.0f : to, kept = __builtin_amdgcn_exp2f(top - base);
+        top = to;
+        sum *= kept;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= kept;
+#pragma unroll
+        for (int b = 0; b < kFlight; ++b) {
+            const float by = part + b < j.parts ? __builtin_amdgcn_exp2f(st[b].x - base) : 0.0f;
+            sum += st[b].y * by;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += x[b][e] * by;
+        }
     }
     if (mine >= j.rows) return;
     const int f = j.row0 + mine, token = f / a.q.group, g = f - token * a.q.group;
@@ -952,6 +961,9 @@ __global__ void __launch_bounds__(WideShape<D>::kWaves * 64) spd_paged_wide_join
 // ---- host ------------------------------------------------------------------------------------------
 
 size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+
+// Requests that a wavefront of the narrow kernel counts, 64 at a time (4,000 of up to 500 tokens, 8 heads on 2: 452 us, and 1,057 by the wide kernel).
+constexpr int kNarrowRequests = 4096;
 
 struct Cut {
     bool wide;
@@ -979,7 +991,11 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
     }
     // A wavefront of the narrow kernel counts the units itself, 64 requests at a time and in 32 bits.
     const double most_units = (double)(rows / kNarrowRows + a.req.n_requests) * (double)((((int64_t)a.req.max_pages << a.cache.page_shift) + kNarrowKeys - 1) / kNarrowKeys + 1);
-    c.wide = rows > 24 * (int64_t)a.req.n_requests || a.req.n_requests > 256 || most_units * a.cache.kv_heads >= 2147483648.0;
+    // It reads a request's keys once for every 16 rows of a key head, which up to some 48 rows costs less than the wide kernel's larger tiles, most of
+    // them empty (16 requests of 4,000 tokens, heads of 64: 32 rows 28 us against 38, 64 rows 44 and 41, 128 rows 83 and 49); and with few rows in all its
+    // smaller pieces fill the chip (one request, 3,000 tokens, 32 heads of 128 on 8: 64 tokens 32 us against 44, 128 49 and 52, 256 81 and 52).
+    c.wide = (rows > 48 * (int64_t)a.req.n_requests && (int64_t)a.req.n_tokens * a.q.heads > 4096) || a.req.n_requests > kNarrowRequests ||
+             most_units * a.cache.kv_heads >= 2147483648.0;
     c.rows = c.wide ? wide_rows(a.head_dim) : kNarrowRows;
     c.keys = c.wide ? wide_keys(a.head_dim) : kNarrowKeys;
     c.threads = c.wide ? 2 * c.rows : 64;

@@ -227,8 +227,8 @@ def test_attention_types_and_layouts(spd, h, shape, dtype, dim, layout, page):
     assert_close(w, run_chunk(spd, h, w, scale=0.2), w.attention(scale=0.2), shape)
 
 
-# requests are counted 64 at a time, by a wavefront up to 256 of them, in LDS up to 1,024
-@pytest.mark.parametrize("n", [64, 65, 200, 256, 257, 1025])
+# requests are counted 64 at a time, by every wavefront up to 4,096 of them, and by one workgroup beyond
+@pytest.mark.parametrize("n", [64, 65, 200, 256, 257, 1025, 4097])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_attention_of_many_requests(spd, h, n, dim):
     rng = np.random.default_rng(n)
@@ -250,6 +250,17 @@ def test_attention_of_long_chunks(spd, h, page, dim, dtype):
         w.table[0, 3], w.table[0, 9 if page < 64 else 5], w.table[1, 1] = -1, w.pages, -7
     print("long chunks", page, dim, flush=True)
     assert_close(w, run_chunk(spd, h, w), w.attention(), "long chunks")
+
+
+@pytest.mark.parametrize("n", [40, 1030])
+def test_attention_of_many_chunks(spd, h, n):
+    """More rows to a request than the kernel for few takes, of requests that are scheduled in LDS and of more."""
+    rng = np.random.default_rng(n)
+    requests = [(int(rng.integers(0, 40)), int(rng.integers(1, 12))) for _ in range(n)]
+    requests[3] = (100, 300)
+    w = World(requests, dim=64, kv_heads=1, group=12, seed=n)
+    print("attention of", n, "chunks", flush=True)
+    assert_close(w, run_chunk(spd, h, w), w.attention(), "%d chunks" % n)
 
 
 def test_attention_over_an_empty_cache(spd, h):
