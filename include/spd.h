@@ -11,7 +11,7 @@
  * an expansion function over row norms (Section 3.4), the others apply their product over
  * the union of the non-zero columns of the two rows (Section 2.2, Eq. 2).  k-NN follows
  * the benchmark protocol of Section 4.2: distances of every query row to every index row,
- * then the k nearest.
+ * then the k nearest.  For programs that answer from what a search found there is attention over a paged cache (further below).
  *
  * Conventions
  *  - Every pointer inside spd_csr and every `out*` pointer is a DEVICE pointer owned by
@@ -271,7 +271,8 @@ spd_status spd_semiring_knn(spd_handle *handle, const spd_csr *Q, const spd_csr 
  *  - Every array is on the DEVICE.  No call reads anything back or waits: lengths and tables are looked at by the kernels, so
  *    the calls can be captured into a graph once the scratch is there (a first call, or spd_set_workspace with
  *    spd_paged_workspace_bytes).  The sizes in the structs are the arrays' and bound every access: lengths and tables that
- *    contradict them give fewer tokens or masked ones, and never an access outside.
+ *    contradict them give fewer tokens or masked ones, and never an access outside.  At most 2^22 requests, 2^28 rows (tokens x heads) to
+ *    append, some 2^31 rows of queries (2^26 where they select pages) and as many tokens to a request.
  *  - A page number outside [0, n_pages) in a block table is a page that is not there: its tokens are masked, and
  *    a new token of it is dropped.  What lies past a request's length, or in pages that no table names, may hold anything, NaN too.
  *    Queries, and keys and values of a request's tokens, must be finite.
@@ -280,7 +281,8 @@ spd_status spd_semiring_knn(spd_handle *handle, const spd_csr *Q, const spd_csr 
 typedef enum { SPD_BF16 = 0, SPD_F16, SPD_DTYPE_COUNT } spd_dtype;
 
 /* page, token in it, key head and place of an element of k: k[page * page_stride + token * token_stride + head * head_stride + place],
- * and of v alike.  Strides are in elements, multiples of 8 (heads may lie before tokens), arrays 16-byte aligned. */
+ * and of v alike.  Strides are in elements, multiples of 8, not negative (heads may lie before tokens, strides may be 0), token_stride below
+ * 2^26; arrays 16-byte aligned. */
 typedef struct {
     spd_dtype dtype;
     int32_t page_size;      /* tokens to a page: a power of two from 16 to 1024 */
@@ -343,7 +345,8 @@ spd_status spd_paged_plan(spd_handle *handle, const spd_paged_step *step);
 spd_status spd_paged_append(spd_handle *handle, const spd_paged_cache *cache, int64_t n_tokens, const spd_rows *k_new,
                             const spd_rows *v_new, const int64_t *slots);
 
-/* Device scratch that one call of spd_paged_attention (`n_select` = 0) or spd_paged_sparse_attention with these sizes needs at most. */
+/* Device scratch that one call of spd_paged_attention (`n_select` = 0) or spd_paged_sparse_attention with these sizes needs at most.  Only the sizes in
+ * `cache` and `batch` are looked at. */
 spd_status spd_paged_workspace_bytes(const spd_handle *handle, const spd_paged_cache *cache, const spd_paged_batch *batch,
                                      int n_heads, int n_select, size_t *bytes);
 
@@ -448,7 +451,8 @@ spd_status spd_set_option(spd_handle *handle, const char *name, int64_t value);
 typedef struct {
     char name[24];        /* "pack_b", "scan", "finalize", "knn_merge"; with the column lists "norms_b",
                                 ("columns", over A's columns) "lists_b", "norms_a", "knn_begin", "scan",
-                                "knn_merge"; a small call: "scan"                                    */
+                                "knn_merge"; a small call: "scan"; over a paged cache "paged_plan",
+                                "paged_append", "paged_select", "paged_attention"                    */
     int32_t rows_per_group; /* scan: R, the rows of A staged together; else 0            */
     int32_t staging_kind; /* scan: 1 dense strip, 2 column-slot strip, 3 hash, 4 Bloom, 5 bitmap,
                                 6 column lists ("match_lists"), 7 none

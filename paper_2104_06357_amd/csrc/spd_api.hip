@@ -1748,7 +1748,9 @@ size_t workspace_bound(const spd_handle *h, const spd_csr *A, const spd_csr *B, 
 }
 // ---- attention over a paged cache ----------------------------------------------------------------
 
-constexpr int64_t kPagedMost = ((int64_t)1 << 31) - 1;        // what the kernels count in 32 bits
+constexpr int64_t kPagedMost = ((int64_t)1 << 31) - 4096;     // what the kernels count in 32 bits, with room for a tile past it
+// What is dealt to workgroups of its own; a launch has fewer than 2^32 threads.
+constexpr int64_t kPagedMostRequests = (int64_t)1 << 22, kPagedMostSelecting = (int64_t)1 << 26, kPagedMostNew = (int64_t)1 << 28;
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -1759,7 +1761,7 @@ spd_status check_paged_cache(spd_handle *h, const spd_paged_cache *c) {
         return fail(h, SPD_ERR_UNSUPPORTED, "page_size must be a power of two from 16 to 1024");
     if (c->head_dim != 64 && c->head_dim != 128) return fail(h, SPD_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
     if (c->n_kv_heads < 1 || c->n_pages < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "cache has no heads or a negative size");
-    if (c->n_kv_heads > 65535 || c->n_pages >= kPagedMost) return fail(h, SPD_ERR_UNSUPPORTED, "more than 65535 key heads or 2^31-2 pages");
+    if (c->n_kv_heads > 65535 || c->n_pages >= kPagedMost) return fail(h, SPD_ERR_UNSUPPORTED, "more than 65535 key heads or 2^31-4097 pages");
     if (c->n_pages > 0 && (!c->k || !c->v)) return fail(h, SPD_ERR_NULL, "k or v of the cache is NULL");
     if (((c->page_stride | c->token_stride | c->head_stride) & 7) != 0 || !aligned16(c->k) || !aligned16(c->v))
         return fail(h, SPD_ERR_UNSUPPORTED, "strides of the cache must be multiples of 8 elements, k and v 16-byte aligned");
@@ -1801,9 +1803,10 @@ spd_status run_paged(spd_handle *h, const spd_paged_cache *c, const spd_paged_ba
     if (b->n_requests < 0 || b->n_tokens < 0 || b->max_pages < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "batch has a negative size");
     if (n_heads < 1 || n_heads % c->n_kv_heads != 0)
         return fail(h, SPD_ERR_DIM_MISMATCH, "n_heads must be a multiple of the cache's n_kv_heads");
-    if (b->n_requests >= kPagedMost || b->n_tokens * (int64_t)n_heads >= kPagedMost || b->n_tokens >= kPagedMost || n_heads > 65535 ||
-        b->max_pages * (int64_t)c->page_size >= kPagedMost)
-        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 requests, rows of queries (tokens x heads) or tokens of a request");
+    if (b->n_requests > kPagedMostRequests) return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^22 requests");
+    if (n_heads > 65535 || b->n_tokens >= kPagedMost / n_heads || b->max_pages >= kPagedMost / c->page_size)
+        return fail(h, SPD_ERR_UNSUPPORTED, "more than 65535 heads, or near 2^31 rows of queries (tokens x heads) or tokens of a request");
+    if (n_select > 0 && b->n_tokens * n_heads > kPagedMostSelecting) return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^26 rows of queries that select pages");
     if (b->n_requests > 1 && b->table_stride < b->max_pages)
         return fail(h, SPD_ERR_DIM_MISMATCH, "rows of block_table overlap (table_stride < max_pages)");
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(h, SPD_ERR_UNSUPPORTED, "scale must be finite and positive");
@@ -2040,7 +2043,7 @@ spd_status spd_paged_plan(spd_handle *h, const spd_paged_step *s) {
     if (s->n_requests > SPD_PAGED_MAX_REQUESTS)
         return fail(h, SPD_ERR_UNSUPPORTED, "more than " + std::to_string(SPD_PAGED_MAX_REQUESTS) + " requests");
     if (s->n_tokens >= kPagedMost || s->max_pages >= kPagedMost || s->n_free >= kPagedMost)
-        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 tokens, pages of a request or free pages");
+        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-4097 tokens, pages of a request or free pages");
     if (s->n_requests > 1 && s->table_stride < s->max_pages)
         return fail(h, SPD_ERR_DIM_MISMATCH, "rows of block_table overlap (table_stride < max_pages)");
     if (!s->query_start || !s->counts || (s->n_requests > 0 && (!s->past_lens || !s->new_lens || !s->kv_lens)) ||
@@ -2061,8 +2064,7 @@ spd_status spd_paged_append(spd_handle *h, const spd_paged_cache *c, int64_t n_t
     spd_status st = check_paged_cache(h, c);
     if (st != SPD_OK) return st;
     if (n_tokens < 0) return fail(h, SPD_ERR_DIM_MISMATCH, "negative number of tokens");
-    if (n_tokens * (int64_t)c->n_kv_heads >= kPagedMost || n_tokens >= kPagedMost)
-        return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^31-2 rows (tokens x heads)");
+    if (n_tokens > kPagedMostNew / c->n_kv_heads) return fail(h, SPD_ERR_UNSUPPORTED, "more than 2^28 rows (tokens x heads)");
     if (n_tokens == 0) return SPD_OK;
     if (!slots) return fail(h, SPD_ERR_NULL, "slots is NULL");
     if ((st = check_paged_rows(h, k_new, "k_new")) != SPD_OK || (st = check_paged_rows(h, v_new, "v_new")) != SPD_OK) return st;
@@ -2078,6 +2080,10 @@ spd_status spd_paged_workspace_bytes(const spd_handle *h, const spd_paged_cache 
     if (!h || !c || !b || !bytes) return SPD_ERR_NULL;
     if (c->n_kv_heads < 1 || n_heads < 1 || n_heads % c->n_kv_heads != 0 || b->n_requests < 0 || b->n_tokens < 0 || b->max_pages < 0)
         return SPD_ERR_DIM_MISMATCH;
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0 || (c->head_dim != 64 && c->head_dim != 128) ||
+        b->n_requests > kPagedMostRequests || n_heads > 65535 || b->n_tokens >= kPagedMost / n_heads || b->max_pages >= kPagedMost / c->page_size)
+        return SPD_ERR_UNSUPPORTED;
+    if (n_select != 0 && (n_select < 2 || n_select > SPD_PAGED_MAX_SELECT)) return SPD_ERR_BAD_K;
     PagedAttention a = paged_attention_args(*c, *b, n_heads);
     a.n_select = n_select;
     a.selected = n_select > 0 ? reinterpret_cast<const int32_t *>(bytes) : nullptr;      // (only looked at for being there)

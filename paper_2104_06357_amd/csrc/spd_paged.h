@@ -30,8 +30,6 @@ struct PagedQueries {
 
 struct PagedOut { void *out; float *lse; };
 
-constexpr int kPagedWave = 64;
-
 hipError_t launch_paged_plan(hipStream_t st, const spd_paged_step &s);
 hipError_t launch_paged_append(hipStream_t st, const spd_paged_cache &c, int64_t n_tokens, const spd_rows &k_new,
                                const spd_rows &v_new, const int64_t *slots);

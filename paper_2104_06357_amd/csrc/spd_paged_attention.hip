@@ -17,7 +17,7 @@ constexpr float kSlack = 8.0f;          // a row's maximum is moved (and its sum
 // another kernel joins them.
 
 struct Tile { int32_t request, row0, units, pad; };
-struct Joined { int32_t parts, request, first_token, position0, row0, rows, head, worker; };     // parts: 0 if there is no such segment
+struct Joined { int32_t parts, worker, first_token, row0, rows, head; };     // parts: 0 if there is no such segment
 struct Schedule {
     int64_t *first;                     // [tiles + 1]: units of the tiles before
     Tile *tiles;
@@ -187,14 +187,19 @@ struct PagePlaces {
 };
 
 // ---- few rows: a wavefront to 16 of them --------------------------------------------------------
-// Decoding, and selected pages: one to 16 rows, and every key is read once.  A wavefront is a worker of its own, and no barrier is in its
-// loop: 32 keys a unit, through 8 KB of LDS, K before V, from where V is read transposed.  The first product is taken as K Q^T and the second as V^T P^T, so that a row's weights leave the first in the
-// lanes and order in which the second takes them, and a row is a lane's, its statistics too.
+// Decoding, and selected pages: one to 16 rows, and every key is read once.  A wavefront streams 32 keys a unit through 8 KB of LDS of its own, K before
+// V, and no barrier is in its loop; the next unit is on its way in registers meanwhile.  The first product is taken as K Q^T and the second as
+// V^T P^T: a row's weights then leave the first in the lanes and, the keys permuted alike on both sides, in the order in which the second
+// takes them, a row's maximum and sum are a lane's (of four that share the keys), and V is read transposed from rows as they lie in memory.
+// Bound by the reading: 48 requests of 500 to 16,000 tokens, 64 heads on 8 of 128, 0.92 GB in 175 us, 5.2 TB/s (a large copy moves 4.95); one
+// request of 2,000 tokens, 8 MB, takes 13 us, most of it the way to its first keys (lengths, table, keys: three round trips).
+// Selected pages that many tokens share come out of L2: 2,048 tokens x 8 heads x 16 pages of 64, 8.6 GB in 440 us, 20 TB/s.  K went straight from
+// memory into the product's operand at first: a row to a lane then, which the vector caches answer with 64 lookups a load where this way has 16.
 
 constexpr int kNarrowRows = 16, kNarrowKeys = 32, kNarrowWaves = 4;
 
 struct NarrowPart {                     // of a segment
-    int request, first_token, count, position0;         // position0: where the request's first new token stands
+    int request, first_token, position0;                // position0: where the request's first new token stands (SELECTED: the token)
     int row0, rows;                     // of the tile in the request: its first, and how many are real
     int head;
     int subs;                           // 16-key steps that a row can see
@@ -435,7 +440,7 @@ struct Narrow {
 __device__ __forceinline__ NarrowPart narrow_part(const PagedAttention &a, const PagedRequest &rq, int request, int row0, int head) {
     NarrowPart p;
     p.request = request;
-    p.first_token = rq.first; p.count = rq.count; p.position0 = rq.kv - rq.count;
+    p.first_token = rq.first; p.position0 = rq.kv - rq.count;
     p.row0 = row0;
     p.rows = min(kNarrowRows, rq.count * a.q.group - row0);
     p.head = head;
@@ -549,7 +554,7 @@ __global__ void __launch_bounds__(kNarrowWaves * 64, 2) spd_paged_narrow_kernel(
         if (unit0 == 0 && unit1 == units) n.write(a, p, team, me);
         else n.leave(s, 2 * (int64_t)w + (unit0 == 0 ? 1 : 0), team, me);
         if (unit0 == 0 && unit1 < units)
-            joined = Joined{(int)(worker_of(all, workers, c.begin + units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, (int)w};
+            joined = Joined{(int)(worker_of(all, workers, c.begin + units - 1) - w) + 1, (int)w, p.first_token, p.row0, p.rows, p.head};
         at = c.begin + unit1;
         if (at < end) c.next(counted, units);
     }
@@ -594,7 +599,7 @@ __device__ __forceinline__ bool selected_part(const PagedAttention &a, int64_t s
     const int r = paged_request_of(a.req, a.cache.page_shift, token, rq);
     if (r < 0) return false;
     p.request = uniform(r);
-    p.first_token = token; p.count = 1;
+    p.first_token = token;
     p.position0 = uniform(rq.kv - rq.count + token - rq.first);
     p.row0 = tile * kNarrowRows;
     p.rows = min(kNarrowRows, a.q.group - p.row0);
@@ -638,7 +643,14 @@ __global__ void __launch_bounds__(64) spd_paged_selected_join_kernel(const Paged
     n.write(a, p, 1, 0);
 }
 
-// ---- many rows: a workgroup to 256 of them -------------------------------------------------------
+// ---- many rows: a workgroup to 128 or 256 of them ------------------------------------------------
+// Prompts: a wavefront has 32 rows, a workgroup's share what is read of K and V, 64 keys a unit, in LDS twice; registers hold the next unit. The
+// products are as above, 32 x 32 of them.  Bound by both kinds of arithmetic, which hardly overlap: with heads of 128 the matrix units are busy for
+// 47 % of the cycles and the vector units for 42 %.  8,192 tokens after 8,192, 32 heads on 8 of 128: 1.61 ms, 1.02 PFLOP/s (a
+// large matrix product reaches 1.58).  Tried and not kept: 64 rows to a wavefront and one of them to a SIMD (3.9 ms: every wait is exposed);
+// a half of the wavefronts half a unit behind the others (1.66); priorities for the products and units of 128 keys (no gain).  Heads of 64 are
+// bound by the exponentials and what goes with them, half the products to each; three workgroups of 4 wavefronts to a compute unit do better there
+// than one of 8 (16 requests of up to 900 new and 4,000 cached tokens, 40 heads on 8: 118 us in all and 145).
 
 template <int D> struct WideShape;
 template <> struct WideShape<128> { static constexpr int kWaves = 8, kKeys = 64, kPerUnit = 2; };
@@ -892,7 +904,7 @@ __global__ void __launch_bounds__(WideShape<D>::kWaves * 64, WideShape<D>::kPerU
         if (p.unit0 == 0 && p.unit1 == t.units) n.write(a, p);
         else n.leave(s, 2 * w + (p.unit0 == 0 ? 1 : 0));
         if (p.unit0 == 0 && p.unit1 < t.units)
-            joined = Joined{(int)(worker_of(all, workers, place.segment_begin + t.units - 1) - w) + 1, p.request, p.first_token, p.position0, p.row0, p.rows, p.head, (int)w};
+            joined = Joined{(int)(worker_of(all, workers, place.segment_begin + t.units - 1) - w) + 1, (int)w, p.first_token, p.row0, p.rows, p.head};
         at = place.segment_begin + p.unit1;
         if (p.unit1 == t.units) {
             place.segment_begin = at;

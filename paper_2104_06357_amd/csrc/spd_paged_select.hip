@@ -108,6 +108,8 @@ __device__ __forceinline__ TokenTile token_tile(const PagedRequests &req, int pa
 // units, 16 pages by 16 tokens, (-w, u) against (lo, hi); a wavefront takes 16 pages a step, so the codes are read
 // once for all tokens of the workgroup.  The scores stay in LDS as keys, and a wavefront chooses for each token.  Where a
 // request has more pages, every 2,048 give their n_select best, and spd_paged_select_join_kernel chooses among those.
+// Bound by latency: one token over 470 pages 9 us (round trips for lengths, page numbers, queries and codes, then the search), 32 requests of up to 938 pages
+// 20 us, 2,048 tokens over 440 to 470 pages 51 us, half of it the search: 20 of its steps of 9 counts.
 template <spd_dtype T, int D>
 __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const PagedAttention a, int32_t *const selected, Candidate *const candidates,
                                                                            const int blocks, const int room) {
