@@ -1,5 +1,6 @@
 // Attention of a chunk of new tokens over a paged cache, over all of its pages or over selected ones.
 #include <algorithm>
+#include <cmath>
 
 #include "spd_paged_device.h"
 
@@ -218,19 +219,38 @@ struct Narrow {
     f32x4 o[kDims];
     float top, sum;
 
+    __device__ __forceinline__ void load_queries(const PagedAttention &a, int token, int head) {
+        const H *const from = (const H *)a.q.ptr + (int64_t)token * a.q.token_stride + (int64_t)head * a.q.head_stride + ((int)threadIdx.x >> 4 & 3) * 8;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) q[s] = *(const H8 *)(from + s * 32);
+    }
+
+    // A row's products with its lane's 8 keys (of 32), -infinity where it does not see one, become weights.  These are rounded to the cache's type, as the
+    // matrix units take them: a relative error of 2^-9 (bf16) or 2^-12 to each, below that of `out`'s own rounding once they are averaged.
+    __device__ __forceinline__ H8 weigh(float *w, float scale) {
+        float big = w[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
+        big = greatest_of_4(big) * scale;
+        if (__any(big > top + kSlack)) {
+            const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+            top = to;
+            sum *= old;
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) o[d] *= old;
+        }
+        const float from = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(w[i], scale, -from)); sum += w[i]; }
+        return rounded<T>(w);
+    }
+
     __device__ __forceinline__ void walk(const PagedAttention &a, const NarrowPart &p, void *lds) {
         const int lane = (int)threadIdx.x & 63, row = lane & 15, quad = lane >> 4;
         const int f = p.row0 + min(row, p.rows - 1), token = SELECTED ? 0 : f / a.q.group, g = SELECTED ? f : f - token * a.q.group;
         const int position = p.position0 + token;
-        {
-            const H *const from = (const H *)a.q.ptr + (int64_t)(p.first_token + token) * a.q.token_stride +
-                                  ((int64_t)p.head * a.q.group + g) * a.q.head_stride + quad * 8;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) q[s] = *(const H8 *)(from + s * 32);
-        }
-#pragma unroll
-        for (int d = 0; d < kDims; ++d) o[d] = f32x4{0, 0, 0, 0};
-        top = -__builtin_inff(); sum = 0.0f;
+        load_queries(a, p.first_token + token, p.head * a.q.group + g);
+        clear();
         const int shift = a.cache.page_shift, per_page = shift - 4;
         // the places of the first row (the least) and of the last
         const int least = p.position0 + (SELECTED ? 0 : p.row0 / a.q.group), most = p.position0 + (SELECTED ? 0 : (p.row0 + p.rows - 1) / a.q.group);
@@ -321,21 +341,7 @@ struct Narrow {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) if (!now_here[j] || now_pos[j] + quad * 4 + i > position) w[j * 4 + i] = -__builtin_inff();
             }
-            float big = w[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
-            big = greatest_of_4(big) * a.q.scale;
-            if (__any(big > top + kSlack)) {
-                const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
-                top = to;
-                sum *= old;
-#pragma unroll
-                for (int d = 0; d < kDims; ++d) o[d] *= old;
-            }
-            const float from = top == -__builtin_inff() ? 0.0f : top;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(w[i], a.q.scale, -from)); sum += w[i]; }
-            const H8 pw = rounded<T>(w);
+            const H8 pw = weigh(w, a.q.scale);
 #pragma unroll
             for (int d = 0; d < kDims; ++d) o[d] = mfma16(read_transposed<T>(tile + (v_lane ^ (d << 5)), 32 * D), pw, o[d]);
         }
@@ -641,6 +647,174 @@ __global__ void __launch_bounds__(64) spd_paged_selected_join_kernel(const Paged
     n.clear();
     n.join_all(s, splits, 0, 1, [&](int i) { return (int64_t)blockIdx.x * splits + i; });
     n.write(a, p, 1, 0);
+}
+
+// Selected pages of many tokens of a request: neighbours choose the same pages more or less, and a page that any of them chose
+// is read once for all.  A workgroup has a key head and 16 wavefronts' tokens, each as many as 16 rows hold; it marks in LDS which wavefronts' tokens chose
+// which page, lists the pages that anybody chose, and goes through them 64 KB at a time: all fetch the next ones, and who chose one of
+// those that are there takes part in it.  Windows of 512 pages, since marks take 32 bytes a page.
+constexpr int kSharedWaves = 16, kSharedPages = 512;
+template <int D> struct SharedShape {
+    static constexpr int kSubs = 1024 / D, kTile = 32 * D * 2;      // steps of 16 keys in a stage; bytes of two of them, of K or V
+    static constexpr int kStage = kSubs / 2 * kTile * 2;            // bytes: K, then V
+    static constexpr size_t kLds = 2 * (size_t)kStage + kSharedPages * (kSharedWaves * 2 + 8) + 64;
+};
+
+template <spd_dtype T, int D>
+__global__ void __launch_bounds__(kSharedWaves * 64) spd_paged_shared_kernel(const PagedAttention a, const int tokens_of_wave, const int blocks) {
+    using H8 = half8_t<T>;
+    using Shape = SharedShape<D>;
+    using N = Narrow<T, D, false>;
+    constexpr int kThreads = kSharedWaves * 64, kSubs = Shape::kSubs, kLoads = 2;
+    extern __shared__ __align__(16) unsigned char s_shared[];
+    uint32_t *const s_marks = (uint32_t *)(s_shared + 2 * Shape::kStage);          // [512][8]: 16 bits to a wavefront
+    int2 *const s_list = (int2 *)(s_marks + kSharedPages * kSharedWaves / 2);      // the pages, ascending: column, number
+    int *const s_count = (int *)(s_list + kSharedPages);                           // [8]
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), row = lane & 15, quad = lane >> 4;
+    // (a key head's workgroups share an XCD)
+    const int64_t grid = (int64_t)gridDim.x, per = grid / 8, rest = grid % 8, xcd = blockIdx.x % 8;
+    const int64_t block = xcd * per + min(xcd, rest) + blockIdx.x / 8;
+    const int tiles = blocks + a.req.n_requests, head = uniform((int)(block / tiles));
+    const TokenTile tile = token_tile(a.req, a.cache.page_shift, uniform((int)(block % tiles)), blocks, tokens_of_wave * kSharedWaves);
+    if (tile.count == 0) return;
+    const int shift = a.cache.page_shift, per_page = shift - 4, group = a.q.group, k = a.n_select;
+    const int position0 = uniform(tile.rq.kv - tile.rq.count + tile.first - tile.rq.first), most = position0 + tile.count - 1;
+    const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride;
+    const int32_t *const chosen = a.selected + ((int64_t)tile.first * a.cache.kv_heads + head) * k;
+    const int64_t token_bytes = a.cache.token_stride * 2;
+    // this wavefront's tokens
+    NarrowPart p{};
+    const int mine0 = wave * tokens_of_wave, mine = min(max(tile.count - mine0, 0), tokens_of_wave);
+    p.first_token = tile.first + min(mine0, tile.count - 1); p.rows = mine * group; p.head = head;
+    const int f = min(row, max(p.rows, 1) - 1), token = f / group, position = position0 + mine0 + token;
+    N n;
+    n.load_queries(a, p.first_token + token, head * group + f - token * group);
+    n.clear();
+    const LdsBytes lds = lds_bytes(s_shared);
+    const int s = lane & 15, k_lane = k_at<D>(row, quad), v_lane = v8_at<D>(quad * 4 + (s >> 2), (s & 3) >> 1) + (s & 1) * 8;
+    // of a stage's rows of K and of V this thread moves two chunks, all of a wavefront in one step of 16 keys
+    const int l_chunk = lane % N::kChunks;
+    H8 kr[kLoads], vr[kLoads];
+    const int pages = most < 0 ? 0 : (most >> shift) + 1;
+#pragma unroll
+    for (int i = 0; i < N::kSteps; ++i) asm volatile("" : "+v"(n.q[i]));           // (there before the loop, which would wait for its own loads with them)
+    for (int page0 = 0; page0 < pages; page0 += kSharedPages) {
+        __syncthreads();
+        for (int i = tid; i < kSharedPages * kSharedWaves / 8; i += kThreads) ((int4 *)s_marks)[i] = int4{0, 0, 0, 0};
+        __syncthreads();
+        for (int i = tid; i < tile.count * k; i += kThreads) {
+            const int t = i / k, col = chosen[(int64_t)t * a.cache.kv_heads * k + (i - t * k)] - page0, w = t / tokens_of_wave;
+            if (col >= 0 && col < kSharedPages) atomicOr(&s_marks[col * (kSharedWaves / 2) + (w >> 1)], 1u << ((w & 1) * 16 + t - w * tokens_of_wave));
+        }
+        __syncthreads();
+        int number = -1, before = 0;
+        if (tid < kSharedPages) {
+            const int4 x = ((const int4 *)s_marks)[tid * 2], y = ((const int4 *)s_marks)[tid * 2 + 1];
+            const bool any = (x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w) != 0 && page0 + tid < a.req.max_pages;
+            if (any) number = table[page0 + tid];
+            if (number >= a.cache.n_pages) number = -1;
+            const uint64_t there = __ballot(number >= 0);
+            before = __popcll(there & (((uint64_t)1 << lane) - 1));
+            if (lane == 0) s_count[wave] = __popcll(there);
+        }
+        __syncthreads();
+        int listed = 0;
+#pragma unroll
+        for (int i = 0; i < kSharedPages / 64; ++i) {
+            const int c = s_count[i];
+            if (i < wave) before += c;
+            listed += c;
+        }
+        if (number >= 0) s_list[before] = make_int2(tid, number);
+        __syncthreads();
+        listed = uniform(listed);
+        const int subs = listed << per_page, stages = (subs + kSubs - 1) / kSubs;
+        auto fetch = [&](int stage) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                // (past the last step the last one again, which nobody looks at: the loads then never wait for one another)
+                const int key = uniform((i * kThreads + wave * 64) / N::kChunks), step = min(stage * kSubs + (key >> 4), subs - 1), r = (key & 15) + lane / N::kChunks;
+                const int2 page = s_list[step >> per_page];
+                const int in = (step & ((1 << per_page) - 1)) << 4;
+                const int64_t at = ((int64_t)uniform(page.y) * a.cache.page_stride + (int64_t)in * a.cache.token_stride + (int64_t)head * a.cache.head_stride) * 2;
+                const int64_t l_at = (int64_t)r * token_bytes + l_chunk * 16;
+                kr[i] = *(const H8 *)((const char *)a.cache.k + at + l_at);
+                vr[i] = *(const H8 *)((const char *)a.cache.v + at + l_at);
+            }
+        };
+        // (values that no token of the tile sees become 0, since 0 times what lies there need not be)
+        auto store = [&](int stage) {
+            const LdsBytes to = lds + (stage & 1) * Shape::kStage;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int key = uniform((i * kThreads + wave * 64) / N::kChunks), step = min(stage * kSubs + (key >> 4), subs - 1), in32 = (key & 31) + lane / N::kChunks;
+                const LdsBytes tile32 = to + (key >> 5) * Shape::kTile;
+                write_row<T>(tile32 + k_at<D>(in32, l_chunk), kr[i]);
+                const int at = ((page0 + s_list[step >> per_page].x) << shift) + ((step & ((1 << per_page) - 1)) << 4);
+                if (at + 15 > most && at + (in32 & 15) > most)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) vr[i][e] = (half_t<T>)0.0f;
+                write_row<T>(tile32 + kSubs / 2 * Shape::kTile + v8_at<D>(in32, l_chunk), vr[i]);
+            }
+        };
+        if (stages > 0) { fetch(0); store(0); }
+        __syncthreads();
+        for (int stage = 0; stage < stages; ++stage) {
+            if (stage + 1 < stages) fetch(stage + 1);
+            // of the stage's steps, one to a lane: which of the wavefront's tokens chose it, and its first key's position
+            int marks = 0, pos = 0;
+            {
+                const int step = stage * kSubs + lane;
+                if (lane < kSubs && step < subs) {
+                    const int col = s_list[step >> per_page].x;
+                    pos = ((page0 + col) << shift) + ((step & ((1 << per_page) - 1)) << 4);
+                    if (mine > 0 && pos <= position0 + mine0 + mine - 1) marks = ((const uint16_t *)s_marks)[col * kSharedWaves + wave];
+                }
+            }
+            const LdsBytes from = lds + (stage & 1) * Shape::kStage;
+            for (uint32_t left = (uint32_t)__ballot(marks != 0); left != 0; ) {
+                const int i = uniform((int)__builtin_ctz(left) >> 1);
+                left &= ~(3u << (2 * i));
+                const LdsBytes tile32 = from + i * Shape::kTile;
+                f32x4 x[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) x[j] = f32x4{0, 0, 0, 0};
+                // (four reads of K and of V are on their way together: the compiler by itself keeps one or two, and more take registers that are not there)
+#pragma unroll
+                for (int st = 0; st < N::kSteps; st += 2) {
+                    H8 kx[2][2];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) kx[h >> 1][h & 1] = read_row<T>(tile32 + (k_lane ^ ((st + (h >> 1)) << 6)) + (h & 1) * 32 * D);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) x[h & 1] = mfma16(kx[h >> 1][h & 1], n.q[st + (h >> 1)], x[h & 1]);
+                }
+                H8 vx[4];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) vx[d] = read_transposed<T>(tile32 + kSubs / 2 * Shape::kTile + (v_lane ^ (d << 5)), 32 * D);
+                __builtin_amdgcn_sched_barrier(0);
+                float w[8];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int m = __builtin_amdgcn_readlane(marks, 2 * i + j), first = __builtin_amdgcn_readlane(pos, 2 * i + j);
+                    const int see = m >> token & 1 ? position - first - quad * 4 : -1;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[j * 4 + e] = e <= see ? x[j][e] : -__builtin_inff();
+                }
+                const H8 pw = n.weigh(w, a.q.scale);
+#pragma unroll
+                for (int d = 0; d < N::kDims; ++d) {
+                    const H8 v = vx[d & 3];
+                    if (d + 4 < N::kDims) vx[d & 3] = read_transposed<T>(tile32 + kSubs / 2 * Shape::kTile + (v_lane ^ ((d + 4) << 5)), 32 * D);
+                    n.o[d] = mfma16(v, pw, n.o[d]);
+                }
+            }
+            if (stage + 1 < stages) store(stage + 1);
+            __syncthreads();
+        }
+    }
+    n.sum = sum_of_4(n.sum);
+    if (mine > 0) n.write(a, p, 1, 0);
 }
 
 // ---- many rows: a workgroup to 128 or 256 of them ------------------------------------------------
@@ -980,7 +1154,7 @@ constexpr int kNarrowRequests = 4096;
 struct Cut {
     bool wide;
     int rows, keys, workers, threads;   // threads: of a worker
-    int splits, head_tiles, team;       // of selected segments
+    int splits, head_tiles, team;       // of selected segments; team 0: tokens share pages, `rows` of them to a wavefront, `tiles` blocks of them
     int64_t tiles;                      // at most
 };
 
@@ -999,6 +1173,14 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
         // up to 8 units of a wavefront cost less than a second launch that joins (4 us)
         c.splits = c.team == 1 ? 1 : (int)std::max<int64_t>(1, std::min(units / (kSelectedTeam * 8), n_cus / segments));
         c.workers = 0;
+        if (a.q.group <= kNarrowRows) {
+            // What a compute unit reads: every token's pages, or those of 16 wavefronts' tokens once, as many as random choices would have in common.
+            const int64_t each = kNarrowRows / a.q.group * kSharedWaves, blocks = (a.req.n_tokens + each - 1) / each, tiles = blocks + a.req.n_requests - 1;
+            const double pages = std::max(a.req.max_pages, 1), tokens = (double)a.req.n_tokens / (double)tiles;
+            const double shared = pages * (1.0 - std::pow(1.0 - std::min(1.0, a.n_select / pages), tokens)) * (double)((tiles * a.cache.kv_heads + n_cus - 1) / n_cus);
+            const double apart = (double)segments / n_cus * a.n_select;
+            if (tiles * a.cache.kv_heads < (1 << 20) && shared * 1.2 < apart) { c.team = 0; c.splits = 1; c.rows = (int)(kNarrowRows / a.q.group); c.tiles = blocks; }
+        }
         return c;
     }
     // A wavefront of the narrow kernel counts the units itself, 64 requests at a time and in 32 bits.
@@ -1043,7 +1225,13 @@ template <spd_dtype T, int D>
 hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Schedule &s) {
     if (a.selected) {
         const int64_t segments = (int64_t)a.req.n_tokens * a.cache.kv_heads * c.head_tiles;
-        if (c.team == 1)
+        if (c.team == 0) {
+            constexpr size_t lds = SharedShape<D>::kLds;
+            const auto kernel = spd_paged_shared_kernel<T, D>;
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((c.tiles + a.req.n_requests) * a.cache.kv_heads)), dim3(kSharedWaves * 64), lds, st, a, c.rows, (int)c.tiles);
+        } else if (c.team == 1)
             hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, 1>), dim3((unsigned)((segments + kNarrowWaves - 1) / kNarrowWaves)),
                                dim3(kNarrowWaves * 64), 0, st, a, s, 1, c.head_tiles);
         else

@@ -91,6 +91,24 @@ __device__ __forceinline__ int paged_request_of(const PagedRequests &q, int page
     return token >= rq.first && token - rq.first < rq.count ? r : -1;
 }
 
+// A tile of up to `each` tokens: workgroups `b` < blocks have the tokens from each * b to the end of the block or of the request that this is in, the others
+// the first tokens of request b - blocks, where it begins inside a block.
+struct TokenTile { int request, first, count; PagedRequest rq; };
+__device__ __forceinline__ TokenTile token_tile(const PagedRequests &req, int page_shift, int b, int blocks, int each) {
+    TokenTile t{-1, 0, 0, {}};
+    if (b < blocks) {
+        t.first = b * each;
+        t.request = paged_request_of(req, page_shift, t.first, t.rq);
+    } else {
+        t.request = b - blocks;
+        t.rq = paged_request(req, page_shift, t.request);
+        t.first = t.rq.first;
+        if (t.first % each == 0) t.request = -1;
+    }
+    if (t.request >= 0) t.count = max(0, min(t.rq.first + t.rq.count, (t.first / each + 1) * each) - t.first);
+    return t;
+}
+
 // ---- matrix products of 16-bit values and their operands -------------------------------------------
 // Lane l of a 32x32x16 product holds, of both operands, row l % 32 and the places (l / 32) * 8 .. + 7 of the contraction, and of the result
 // column l % 32 and rows 8 (i / 4) + 4 (l / 32) + i % 4, i = 0 .. 15; of a 16x16x32 product row l % 16 and places (l / 16) * 8 .. + 7, and column

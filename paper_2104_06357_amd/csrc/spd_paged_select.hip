@@ -86,24 +86,6 @@ __device__ __forceinline__ void choose(int n, int k, int each, Key key, Take tak
 
 struct Candidate { uint32_t key; int32_t page; };
 
-// A tile of tokens: workgroups `b` < blocks have the tokens from 16 b to the end of the block or of the request that 16 b is in, the others
-// the first tokens of request b - blocks, where it begins inside a block.
-struct TokenTile { int request, first, count; PagedRequest rq; };
-__device__ __forceinline__ TokenTile token_tile(const PagedRequests &req, int page_shift, int b, int blocks) {
-    TokenTile t{-1, 0, 0, {}};
-    if (b < blocks) {
-        t.first = b * kSelectTokens;
-        t.request = paged_request_of(req, page_shift, t.first, t.rq);
-    } else {
-        t.request = b - blocks;
-        t.rq = paged_request(req, page_shift, t.request);
-        t.first = t.rq.first;
-        if (t.first % kSelectTokens == 0) t.request = -1;
-    }
-    if (t.request >= 0) t.count = max(0, min(t.rq.first + t.rq.count, (t.first / kSelectTokens + 1) * kSelectTokens) - t.first);
-    return t;
-}
-
 // Up to 16 tokens of a request against up to 2,048 of its pages, in one key head.  Both sides' 8-bit codes go through the matrix
 // units, 16 pages by 16 tokens, (-w, u) against (lo, hi); a wavefront takes 16 pages a step, so the codes are read
 // once for all tokens of the workgroup.  The scores stay in LDS as keys, and a wavefront chooses for each token.  Where a
@@ -118,7 +100,7 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
     extern __shared__ __align__(16) uint32_t s_key[];             // [16][room]
     __shared__ __align__(16) int8_t s_code[kSelectTokens][2 * D];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kvh = (int)blockIdx.y, group = a.q.group, chunk = (int)blockIdx.z;
-    const TokenTile tile = token_tile(a.req, a.cache.page_shift, (int)blockIdx.x, blocks);
+    const TokenTile tile = token_tile(a.req, a.cache.page_shift, (int)blockIdx.x, blocks, kSelectTokens);
     if (tile.count == 0) return;
     const PagedRequest &rq = tile.rq;
     const int position0 = rq.kv - rq.count + tile.first - rq.first, shift = a.cache.page_shift;

@@ -440,6 +440,40 @@ def test_sparse_of_many_tokens_and_a_wide_table(spd, h):
     check_sparse(spd, h, w, 16, "many pages")
 
 
+@pytest.mark.parametrize("group,kv_heads,dtype,dim,page,layout", [(1, 16, "bf16", 64, 16, "thd"), (3, 8, "f16", 128, 32, "htd"),
+                                                                  (4, 8, "bf16", 128, 64, "thd"), (5, 8, "bf16", 64, 64, "htd"),
+                                                                  (8, 8, "f16", 64, 16, "thd"), (16, 8, "bf16", 128, 16, "thd")])
+def test_sparse_tokens_that_share_pages(spd, h, group, kv_heads, dtype, dim, page, layout):
+    """So many tokens of a request that a page is read once for all that chose it: tiles of tokens that end inside a request or hold one token."""
+    w = World([(13 * page + 5, 273), (0, 1), (6, 130), (0, 0), (2 * page - 1, 65)], group=group, kv_heads=kv_heads, dtype=dtype, dim=dim,
+              page=page, layout=layout, seed=group, drift=0.7, fused=True)
+    print("shared", group, kv_heads, dtype, dim, page, flush=True)
+    check_sparse(spd, h, w, 8, "shared pages")
+
+
+def test_sparse_tokens_that_share_pages_larger_than_a_stage(spd, h):
+    w = World([(2000, 200), (500, 31)], group=4, kv_heads=8, page=1024, seed=3, drift=0.7)
+    check_sparse(spd, h, w, 3, "shared pages of 1,024")
+
+
+def test_sparse_tokens_that_share_pages_of_a_long_request(spd, h):
+    """More pages than are marked at a time."""
+    w = World([(16 * 1030 + 3, 210)], group=16, kv_heads=16, dim=64, page=16, seed=4, drift=0.7)
+    check_sparse(spd, h, w, 64, "shared pages of a long request")
+
+
+def test_sparse_tokens_that_share_pages_that_are_not_there(spd, h):
+    w = World([(300, 200), (40, 150), (10, 30)], group=4, kv_heads=8, page=16, seed=6, drift=0.7)
+    w.make_bounds()
+    w.table[0, [0, 3, 17, 31]] = torch.tensor([-1, w.pages, 2 ** 31 - 1, -(2 ** 31)], dtype=torch.int32)
+    w.table[1, 2] = -5
+    w.kv_lens[2] = 17                                   # fewer than there are new tokens
+    out, lse, selected = h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 9)
+    want = w.selection(9)
+    assert torch.equal(selected.cpu(), want)
+    assert_close(w, (out, lse), w.attention(selected=want), "shared pages that are not there")
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def serve(spd, h, steps, seed, n_select=0):
