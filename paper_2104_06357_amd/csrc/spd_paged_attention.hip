@@ -225,13 +225,8 @@ struct Narrow {
         for (int s = 0; s < kSteps; ++s) q[s] = *(const H8 *)(from + s * 32);
     }
 
-    // A row's products with its lane's 8 keys (of 32), -infinity where it does not see one, become weights.  These are rounded to the cache's type, as the
-    // matrix units take them: a relative error of 2^-9 (bf16) or 2^-12 to each, below that of `out`'s own rounding once they are averaged.
-    __device__ __forceinline__ H8 weigh(float *w, float scale) {
-        float big = w[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
-        big = greatest_of_4(big) * scale;
+    // Of a row's maximum over new keys; the sums follow it only once it has grown by more than kSlack.
+    __device__ __forceinline__ void move_top(float big) {
         if (__any(big > top + kSlack)) {
             const float to = fmaxf(top, big), old = to == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(top - to);
             top = to;
@@ -239,6 +234,15 @@ struct Narrow {
 #pragma unroll
             for (int d = 0; d < kDims; ++d) o[d] *= old;
         }
+    }
+
+    // A row's products with its lane's 8 keys (of 32), -infinity where it does not see one, become weights.  These are rounded to the cache's type, as the
+    // matrix units take them: a relative error of 2^-9 (bf16) or 2^-12 to each, below that of `out`'s own rounding once they are averaged.
+    __device__ __forceinline__ H8 weigh(float *w, float scale) {
+        float big = w[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) big = fmaxf(big, w[i]);
+        move_top(greatest_of_4(big) * scale);
         const float from = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
         for (int i = 0; i < 8; ++i) { w[i] = __builtin_amdgcn_exp2f(fmaf(w[i], scale, -from)); sum += w[i]; }
@@ -650,61 +654,59 @@ __global__ void __launch_bounds__(64) spd_paged_selected_join_kernel(const Paged
 }
 
 // Selected pages of many tokens of a request: neighbours choose the same pages more or less, and a page that any of them chose
-// is read once for all.  A workgroup has a key head and 16 wavefronts' tokens, each as many as 16 rows hold; it marks in LDS which wavefronts' tokens chose
-// which page, lists the pages that anybody chose, and goes through them 64 KB at a time: all fetch the next ones, and who chose one of
-// those that are there takes part in it.  Windows of 512 pages, since marks take 32 bytes a page.
-constexpr int kSharedWaves = 16, kSharedPages = 512;
+// is read once for all.  A workgroup has a key head and 16 tiles of tokens, each as many as 16 rows hold; it marks in LDS which tiles' tokens chose
+// which page, lists the pages that anybody chose, and goes through them 64 keys a block.  4 wavefronts move the blocks into a ring of 128 KB, 8 with two
+// tiles each take part in those that their tokens chose, and each goes on as far as the ring lets it: with a barrier after every 128 keys all of them waited
+// for the one that had the most to do.  Windows of 512 pages, since marks take 32 bytes a page.
+constexpr int kSharedTiles = 16, kSharedReaders = 8, kSharedMovers = 4, kSharedPages = 512, kSharedThreads = (kSharedReaders + kSharedMovers) * 64;
 template <int D> struct SharedShape {
-    static constexpr int kSubs = 1024 / D, kTile = 32 * D * 2;      // steps of 16 keys in a stage; bytes of two of them, of K or V
-    static constexpr int kStage = kSubs / 2 * kTile * 2;            // bytes: K, then V
-    static constexpr size_t kLds = 2 * (size_t)kStage + kSharedPages * (kSharedWaves * 2 + 8) + 64;
+    static constexpr int kHalf = 32 * D * 2, kBlock = 4 * kHalf, kRing = 128 * 1024 / kBlock;      // bytes of 32 keys' K or V, and of a block: K, then V
+    static constexpr size_t kLds = (size_t)kRing * kBlock + kSharedPages * (kSharedTiles * 2 + 8) + 128;
 };
 
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kSharedWaves * 64) spd_paged_shared_kernel(const PagedAttention a, const int tokens_of_wave, const int blocks) {
+__global__ void __launch_bounds__(kSharedThreads) spd_paged_shared_kernel(const PagedAttention a, const int tokens_of_tile, const int blocks) {
     using H8 = half8_t<T>;
     using Shape = SharedShape<D>;
     using N = Narrow<T, D, false>;
-    constexpr int kThreads = kSharedWaves * 64, kSubs = Shape::kSubs, kLoads = 2;
     extern __shared__ __align__(16) unsigned char s_shared[];
-    uint32_t *const s_marks = (uint32_t *)(s_shared + 2 * Shape::kStage);          // [512][8]: 16 bits to a wavefront
-    int2 *const s_list = (int2 *)(s_marks + kSharedPages * kSharedWaves / 2);      // the pages, ascending: column, number
-    int *const s_count = (int *)(s_list + kSharedPages);                           // [8]
+    uint32_t *const s_marks = (uint32_t *)(s_shared + (size_t)Shape::kRing * Shape::kBlock);     // [512][8]: 16 bits to a tile
+    int2 *const s_list = (int2 *)(s_marks + kSharedPages * kSharedTiles / 2);       // the pages, ascending: column, number
+    int *const s_count = (int *)(s_list + kSharedPages);                            // [8]
+    int *const s_moved = s_count + 8, *const s_read = s_moved + kSharedMovers;      // blocks up to which each mover, and each reader, is done
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), row = lane & 15, quad = lane >> 4;
     // (a key head's workgroups share an XCD)
     const int64_t grid = (int64_t)gridDim.x, per = grid / 8, rest = grid % 8, xcd = blockIdx.x % 8;
-    const int64_t block = xcd * per + min(xcd, rest) + blockIdx.x / 8;
-    const int tiles = blocks + a.req.n_requests, head = uniform((int)(block / tiles));
-    const TokenTile tile = token_tile(a.req, a.cache.page_shift, uniform((int)(block % tiles)), blocks, tokens_of_wave * kSharedWaves);
-    if (tile.count == 0) return;
+    const int64_t group_number = xcd * per + min(xcd, rest) + blockIdx.x / 8;
+    const int tiles = blocks + a.req.n_requests, head = uniform((int)(group_number / tiles));
+    const TokenTile all = token_tile(a.req, a.cache.page_shift, uniform((int)(group_number % tiles)), blocks, tokens_of_tile * kSharedTiles);
+    if (all.count == 0) return;
     const int shift = a.cache.page_shift, per_page = shift - 4, group = a.q.group, k = a.n_select;
-    const int position0 = uniform(tile.rq.kv - tile.rq.count + tile.first - tile.rq.first), most = position0 + tile.count - 1;
-    const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride;
-    const int32_t *const chosen = a.selected + ((int64_t)tile.first * a.cache.kv_heads + head) * k;
-    const int64_t token_bytes = a.cache.token_stride * 2;
-    // this wavefront's tokens
-    NarrowPart p{};
-    const int mine0 = wave * tokens_of_wave, mine = min(max(tile.count - mine0, 0), tokens_of_wave);
-    p.first_token = tile.first + min(mine0, tile.count - 1); p.rows = mine * group; p.head = head;
-    const int f = min(row, max(p.rows, 1) - 1), token = f / group, position = position0 + mine0 + token;
-    N n;
-    n.load_queries(a, p.first_token + token, head * group + f - token * group);
-    n.clear();
-    const LdsBytes lds = lds_bytes(s_shared);
-    const int s = lane & 15, k_lane = k_at<D>(row, quad), v_lane = v8_at<D>(quad * 4 + (s >> 2), (s & 3) >> 1) + (s & 1) * 8;
-    // of a stage's rows of K and of V this thread moves two chunks, all of a wavefront in one step of 16 keys
-    const int l_chunk = lane % N::kChunks;
-    H8 kr[kLoads], vr[kLoads];
+    const int position0 = uniform(all.rq.kv - all.rq.count + all.first - all.rq.first), most = position0 + all.count - 1;
+    const int32_t *const table = a.req.block_table + (int64_t)all.request * a.req.table_stride;
+    const int32_t *const chosen = a.selected + ((int64_t)all.first * a.cache.kv_heads + head) * k;
+    const LdsBytes ring = lds_bytes(s_shared);
+
+    auto wait_for = [&](const int *done, int many, int block) {           // until each of them is
+        while (!__all(__hip_atomic_load(done + (lane & (many - 1)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) >= block)) ;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    };
+    auto is_done = [&](int *done, int block) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        if (lane == 0) __hip_atomic_store(done, block, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
+
     const int pages = most < 0 ? 0 : (most >> shift) + 1;
-#pragma unroll
-    for (int i = 0; i < N::kSteps; ++i) asm volatile("" : "+v"(n.q[i]));           // (there before the loop, which would wait for its own loads with them)
-    for (int page0 = 0; page0 < pages; page0 += kSharedPages) {
+    // The steps of 16 keys that the list of the pages from page0 on holds.  (All wavefronts come here, movers and readers from loops of their own: what
+    // the ones hold then takes no registers of the others.)
+    auto list_pages = [&](int page0) {
         __syncthreads();
-        for (int i = tid; i < kSharedPages * kSharedWaves / 8; i += kThreads) ((int4 *)s_marks)[i] = int4{0, 0, 0, 0};
+        for (int i = tid; i < kSharedPages * kSharedTiles / 8; i += kSharedThreads) ((int4 *)s_marks)[i] = int4{0, 0, 0, 0};
+        if (tid < kSharedMovers + kSharedReaders) s_moved[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < tile.count * k; i += kThreads) {
-            const int t = i / k, col = chosen[(int64_t)t * a.cache.kv_heads * k + (i - t * k)] - page0, w = t / tokens_of_wave;
-            if (col >= 0 && col < kSharedPages) atomicOr(&s_marks[col * (kSharedWaves / 2) + (w >> 1)], 1u << ((w & 1) * 16 + t - w * tokens_of_wave));
+        for (int i = tid; i < all.count * k; i += kSharedThreads) {
+            const int t = i / k, col = chosen[(int64_t)t * a.cache.kv_heads * k + (i - t * k)] - page0, w = t / tokens_of_tile;
+            if (col >= 0 && col < kSharedPages) atomicOr(&s_marks[col * (kSharedTiles / 2) + (w >> 1)], 1u << ((w & 1) * 16 + t - w * tokens_of_tile));
         }
         __syncthreads();
         int number = -1, before = 0;
@@ -727,94 +729,165 @@ __global__ void __launch_bounds__(kSharedWaves * 64) spd_paged_shared_kernel(con
         }
         if (number >= 0) s_list[before] = make_int2(tid, number);
         __syncthreads();
-        listed = uniform(listed);
-        const int subs = listed << per_page, stages = (subs + kSubs - 1) / kSubs;
-        auto fetch = [&](int stage) {
+        return uniform(listed) << per_page;
+    };
+    if (wave >= kSharedReaders) {
+        // 16 keys of every block; past the last of all the last ones again, which nobody looks at
+        constexpr int kLoads = N::kLoads / 2, kRows = N::kRowsOfLoad;
+        const int me = wave - kSharedReaders, l_row = lane / N::kChunks, l_chunk = lane % N::kChunks;
+        const int64_t l_at = (int64_t)l_row * a.cache.token_stride * 2 + l_chunk * 16;
+        struct Step { H8 k[kLoads], v[kLoads]; int at; };
+        auto load = [&](int page0, int subs, int block, Step &x) {
+            const int step = min(block * 4 + me, subs - 1), in = (step & ((1 << per_page) - 1)) << 4;
+            const int2 page = s_list[step >> per_page];
+            x.at = uniform(((page0 + page.x) << shift) + in);
+            const int64_t from = ((int64_t)uniform(page.y) * a.cache.page_stride + (int64_t)in * a.cache.token_stride + (int64_t)head * a.cache.head_stride) * 2;
+            const char *const kp = (const char *)a.cache.k + from, *const vp = (const char *)a.cache.v + from;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) x.k[i] = *(const H8 *)(kp + (int64_t)(i * kRows) * a.cache.token_stride * 2 + l_at);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) x.v[i] = *(const H8 *)(vp + (int64_t)(i * kRows) * a.cache.token_stride * 2 + l_at);
+        };
+        auto store = [&](int block, Step &x) {
+            wait_for(s_read, kSharedReaders, block - Shape::kRing + 1);
+            const LdsBytes to = ring + (block % Shape::kRing) * Shape::kBlock + (me >> 1) * Shape::kHalf;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                // (past the last step the last one again, which nobody looks at: the loads then never wait for one another)
-                const int key = uniform((i * kThreads + wave * 64) / N::kChunks), step = min(stage * kSubs + (key >> 4), subs - 1), r = (key & 15) + lane / N::kChunks;
-                const int2 page = s_list[step >> per_page];
-                const int in = (step & ((1 << per_page) - 1)) << 4;
-                const int64_t at = ((int64_t)uniform(page.y) * a.cache.page_stride + (int64_t)in * a.cache.token_stride + (int64_t)head * a.cache.head_stride) * 2;
-                const int64_t l_at = (int64_t)r * token_bytes + l_chunk * 16;
-                kr[i] = *(const H8 *)((const char *)a.cache.k + at + l_at);
-                vr[i] = *(const H8 *)((const char *)a.cache.v + at + l_at);
+                const int r = (me & 1) * 16 + i * kRows + l_row;
+                write_row<T>(to + k_at<D>(r, l_chunk), x.k[i]);
+                // (values that no token of the workgroup sees become 0, since 0 times what lies there need not be)
+                if (x.at + 15 > most && x.at + i * kRows + l_row > most)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x.v[i][e] = (half_t<T>)0.0f;
+                write_row<T>(to + 2 * Shape::kHalf + v8_at<D>(r, l_chunk), x.v[i]);
             }
+            is_done(s_moved + me, block + 1);
         };
-        // (values that no token of the tile sees become 0, since 0 times what lies there need not be)
-        auto store = [&](int stage) {
-            const LdsBytes to = lds + (stage & 1) * Shape::kStage;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const int key = uniform((i * kThreads + wave * 64) / N::kChunks), step = min(stage * kSubs + (key >> 4), subs - 1), in32 = (key & 31) + lane / N::kChunks;
-                const LdsBytes tile32 = to + (key >> 5) * Shape::kTile;
-                write_row<T>(tile32 + k_at<D>(in32, l_chunk), kr[i]);
-                const int at = ((page0 + s_list[step >> per_page].x) << shift) + ((step & ((1 << per_page) - 1)) << 4);
-                if (at + 15 > most && at + (in32 & 15) > most)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) vr[i][e] = (half_t<T>)0.0f;
-                write_row<T>(tile32 + kSubs / 2 * Shape::kTile + v8_at<D>(in32, l_chunk), vr[i]);
+        for (int page0 = 0; page0 < pages; page0 += kSharedPages) {
+            const int subs = list_pages(page0), n_blocks = (subs + 3) / 4;
+            if (subs == 0) continue;
+            Step x, y;
+            load(page0, subs, 0, x);
+            for (int block = 0; block < n_blocks; block += 2) {
+                load(page0, subs, block + 1, y);
+                store(block, x);
+                load(page0, subs, block + 2, x);
+                if (block + 1 < n_blocks) store(block + 1, y);
             }
-        };
-        if (stages > 0) { fetch(0); store(0); }
-        __syncthreads();
-        for (int stage = 0; stage < stages; ++stage) {
-            if (stage + 1 < stages) fetch(stage + 1);
-            // of the stage's steps, one to a lane: which of the wavefront's tokens chose it, and its first key's position
-            int marks = 0, pos = 0;
-            {
-                const int step = stage * kSubs + lane;
-                if (lane < kSubs && step < subs) {
-                    const int col = s_list[step >> per_page].x;
-                    pos = ((page0 + col) << shift) + ((step & ((1 << per_page) - 1)) << 4);
-                    if (mine > 0 && pos <= position0 + mine0 + mine - 1) marks = ((const uint16_t *)s_marks)[col * kSharedWaves + wave];
-                }
-            }
-            const LdsBytes from = lds + (stage & 1) * Shape::kStage;
-            for (uint32_t left = (uint32_t)__ballot(marks != 0); left != 0; ) {
-                const int i = uniform((int)__builtin_ctz(left) >> 1);
-                left &= ~(3u << (2 * i));
-                const LdsBytes tile32 = from + i * Shape::kTile;
-                f32x4 x[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) x[j] = f32x4{0, 0, 0, 0};
-                // (four reads of K and of V are on their way together: the compiler by itself keeps one or two, and more take registers that are not there)
-#pragma unroll
-                for (int st = 0; st < N::kSteps; st += 2) {
-                    H8 kx[2][2];
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) kx[h >> 1][h & 1] = read_row<T>(tile32 + (k_lane ^ ((st + (h >> 1)) << 6)) + (h & 1) * 32 * D);
-                    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) x[h & 1] = mfma16(kx[h >> 1][h & 1], n.q[st + (h >> 1)], x[h & 1]);
-                }
-                H8 vx[4];
-#pragma unroll
-                for (int d = 0; d < 4; ++d) vx[d] = read_transposed<T>(tile32 + kSubs / 2 * Shape::kTile + (v_lane ^ (d << 5)), 32 * D);
-                __builtin_amdgcn_sched_barrier(0);
-                float w[8];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int m = __builtin_amdgcn_readlane(marks, 2 * i + j), first = __builtin_amdgcn_readlane(pos, 2 * i + j);
-                    const int see = m >> token & 1 ? position - first - quad * 4 : -1;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[j * 4 + e] = e <= see ? x[j][e] : -__builtin_inff();
-                }
-                const H8 pw = n.weigh(w, a.q.scale);
-#pragma unroll
-                for (int d = 0; d < N::kDims; ++d) {
-                    const H8 v = vx[d & 3];
-                    if (d + 4 < N::kDims) vx[d & 3] = read_transposed<T>(tile32 + kSubs / 2 * Shape::kTile + (v_lane ^ ((d + 4) << 5)), 32 * D);
-                    n.o[d] = mfma16(v, pw, n.o[d]);
-                }
-            }
-            if (stage + 1 < stages) store(stage + 1);
-            __syncthreads();
         }
+        return;
     }
-    n.sum = sum_of_4(n.sum);
-    if (mine > 0) n.write(a, p, 1, 0);
+    // a reader's two tiles
+    N n[2];
+    const int token = min(row, tokens_of_tile * group - 1) / group;
+    int tile_last[2], position[2];                      // the last position that a tile sees, and its row's own
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int from = (wave * 2 + t) * tokens_of_tile, mine = min(max(all.count - from, 0), tokens_of_tile);
+        tile_last[t] = mine > 0 ? position0 + from + mine - 1 : -1;
+        position[t] = position0 + from + token;
+        n[t].clear();
+        n[t].load_queries(a, all.first + min(from + token, all.count - 1), head * group + min(row, tokens_of_tile * group - 1) - token * group);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < N::kSteps; ++i) asm volatile("" : "+v"(n[t].q[i]));     // (there before the loop)
+    const int k_of_lane = k_at<D>(row, quad), v_of_lane = v8_at<D>(quad * 4 + (row >> 2), (row & 3) >> 1) + (row & 1) * 8;
+    // Takes in 32 keys for a tile: K at `at`, of two steps the first keys' positions and who chose them.  A page that is not a row's own counts for it
+    // as a whole or not at all.
+    auto take = [&](N &r, int least, int position, LdsBytes at, const int *first, const bool *mine) {
+        int k_lane = k_of_lane, v_lane = v_of_lane;
+        asm volatile("" : "+v"(k_lane), "+v"(v_lane));  // (their variants are made here, or a dozen registers hold them throughout)
+        f32x4 x[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) x[j] = f32x4{0, 0, 0, 0};
+        // (K as a whole and half of V are on their way together: the compiler by itself keeps one or two reads)
+        H8 kx[N::kSteps][2], vx[4];
+#pragma unroll
+        for (int st = 0; st < N::kSteps; ++st)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) kx[st][j] = read_row<T>(at + (k_lane ^ (st << 6)) + j * 32 * D);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int st = 0; st < N::kSteps; ++st)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) x[j] = mfma16(kx[st][j], r.q[st], x[j]);
+        const LdsBytes v_at = at + 2 * Shape::kHalf;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) vx[d] = read_transposed<T>(v_at + (v_lane ^ (d << 5)), 32 * D);
+        __builtin_amdgcn_sched_barrier(0);
+        float big = -__builtin_inff(), w[8];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (first[j] + 15 > least)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (first[j] + quad * 4 + e > position) x[j][e] = -__builtin_inff();
+            const float of = fmaxf(fmaxf(x[j][0], x[j][1]), fmaxf(x[j][2], x[j][3]));
+            big = fmaxf(big, mine[j] ? of : -__builtin_inff());
+        }
+        r.move_top(greatest_of_4(big) * a.q.scale);
+        const float top = r.top == -__builtin_inff() ? 0.0f : r.top;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float from = mine[j] ? -top : -__builtin_inff();
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { w[4 * j + e] = __builtin_amdgcn_exp2f(fmaf(x[j][e], a.q.scale, from)); r.sum += w[4 * j + e]; }
+        }
+        const H8 pw = rounded<T>(w);
+#pragma unroll
+        for (int d = 0; d < N::kDims; ++d) {
+            const H8 v = vx[d & 3];
+            if (d + 4 < N::kDims) vx[d & 3] = read_transposed<T>(v_at + (v_lane ^ ((d + 4) << 5)), 32 * D);
+            r.o[d] = mfma16(v, pw, r.o[d]);
+        }
+    };
+    for (int page0 = 0; page0 < pages; page0 += kSharedPages) {
+        const int subs = list_pages(page0);
+        for (int step0 = 0; step0 < subs; step0 += 64) {
+            // of 64 steps of 16 keys, one to a lane: which tokens chose it, 16 bits to a tile, and its first key's position
+            uint32_t marks = 0;
+            int pos = 0x7fffff00;                       // past the last step: behind every position, which masks what is there instead
+            if (step0 + lane < subs) {
+                const int col = s_list[(step0 + lane) >> per_page].x;
+                pos = ((page0 + col) << shift) + (((step0 + lane) & ((1 << per_page) - 1)) << 4);
+                marks = s_marks[col * (kSharedTiles / 2) + wave];
+                if (pos > tile_last[0]) marks &= 0xffff0000u;
+                if (pos > tile_last[1]) marks &= 0xffffu;
+            }
+            const uint64_t who[2] = {__ballot((marks & 0xffffu) != 0), __ballot((marks >> 16) != 0)};
+            for (uint64_t left = who[0] | who[1]; left != 0; ) {
+                const int i = uniform((int)__builtin_ctzll(left) >> 2), block = step0 / 4 + i;
+                left &= ~((uint64_t)15 << (4 * i));
+                is_done(s_read + wave, block);
+                wait_for(s_moved, kSharedMovers, block + 1);
+                const LdsBytes at = ring + (block % Shape::kRing) * Shape::kBlock;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll 1
+                    for (int half = 0; half < 2; ++half) {
+                        if ((who[t] >> (4 * i + 2 * half) & 3) == 0) continue;
+                        int first[2];
+                        bool mine[2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            first[j] = __builtin_amdgcn_readlane(pos, 4 * i + 2 * half + j);
+                            mine[j] = (uint32_t)__builtin_amdgcn_readlane((int)marks, 4 * i + 2 * half + j) >> (16 * t) >> token & 1;
+                        }
+                        take(n[t], position0 + (wave * 2 + t) * tokens_of_tile, position[t], at + half * Shape::kHalf, first, mine);
+                    }
+            }
+        }
+        is_done(s_read + wave, 0x7fffffff);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int from = (wave * 2 + t) * tokens_of_tile, mine = min(max(all.count - from, 0), tokens_of_tile);
+        NarrowPart p{};
+        p.first_token = all.first + from; p.rows = mine * group; p.head = head;
+        n[t].sum = sum_of_4(n[t].sum);
+        if (mine > 0) n[t].write(a, p, 1, 0);
+    }
 }
 
 // ---- many rows: a workgroup to 128 or 256 of them ------------------------------------------------
@@ -1154,7 +1227,7 @@ constexpr int kNarrowRequests = 4096;
 struct Cut {
     bool wide;
     int rows, keys, workers, threads;   // threads: of a worker
-    int splits, head_tiles, team;       // of selected segments; team 0: tokens share pages, `rows` of them to a wavefront, `tiles` blocks of them
+    int splits, head_tiles, team;       // of selected segments; team 0: tokens share pages, `rows` of them to a tile, `tiles` workgroups of 16 tiles
     int64_t tiles;                      // at most
 };
 
@@ -1174,12 +1247,20 @@ Cut cut_of(const PagedAttention &a, int n_cus) {
         c.splits = c.team == 1 ? 1 : (int)std::max<int64_t>(1, std::min(units / (kSelectedTeam * 8), n_cus / segments));
         c.workers = 0;
         if (a.q.group <= kNarrowRows) {
-            // What a compute unit reads: every token's pages, or those of 16 wavefronts' tokens once, as many as random choices would have in common.
-            const int64_t each = kNarrowRows / a.q.group * kSharedWaves, blocks = (a.req.n_tokens + each - 1) / each, tiles = blocks + a.req.n_requests - 1;
-            const double pages = std::max(a.req.max_pages, 1), tokens = (double)a.req.n_tokens / (double)tiles;
-            const double shared = pages * (1.0 - std::pow(1.0 - std::min(1.0, a.n_select / pages), tokens)) * (double)((tiles * a.cache.kv_heads + n_cus - 1) / n_cus);
-            const double apart = (double)segments / n_cus * a.n_select;
-            if (tiles * a.cache.kv_heads < (1 << 20) && shared * 1.2 < apart) { c.team = 0; c.splits = 1; c.rows = (int)(kNarrowRows / a.q.group); c.tiles = blocks; }
+            // In halves of a block (32 keys) that a compute unit goes through: every segment's one after the other; or, shared, what is moved into the ring and
+            // what a reader's two tiles take, where any of their tokens chose it, as often as random choices would meet.  Taking one costs 4.2 times
+            // as much as one of a segment does, since a page that 1 of 4 tokens chose fills 4 rows of 16 and the readers wait for one another: 2,048
+            // tokens, 16 of 470 pages of 64, 32 heads on 8: 300 us against 454; 1,024 264 and 232; heads of 64 201 and 240; page 16, 64 of them, 398
+            // and 285; 8 heads on 8 577 and 268; 4 requests of 600 tokens after 3,000 244 and 485.
+            const double pages = std::max(a.req.max_pages, 1), miss = 1.0 - std::min(1.0, a.n_select / pages), of_page = (double)(1 << a.cache.page_shift) / kNarrowKeys;
+            const int64_t of_tile = kNarrowRows / a.q.group, each = of_tile * kSharedTiles, blocks = (a.req.n_tokens + each - 1) / each, tiles = blocks + a.req.n_requests - 1;
+            const int64_t rounds = (tiles * a.cache.kv_heads + n_cus - 1) / n_cus;
+            const double tokens = (double)a.req.n_tokens / (double)tiles, moved = pages * of_page * (1.0 - std::pow(miss, tokens));
+            const double taken = 2 * pages * of_page * (1.0 - std::pow(miss, std::min((double)of_tile, tokens) * std::max(1.0, 1.0 / of_page)));
+            const double apart = (double)segments / n_cus * a.n_select * of_page;
+            if (tiles * a.cache.kv_heads < (1 << 20) && rounds * std::max(moved, 4.2 * taken) < apart) {
+                c.team = 0; c.splits = 1; c.rows = (int)of_tile; c.tiles = blocks;
+            }
         }
         return c;
     }
@@ -1230,7 +1311,7 @@ hipError_t start(hipStream_t st, const PagedAttention &a, const Cut &c, const Sc
             const auto kernel = spd_paged_shared_kernel<T, D>;
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) return e;
-            hipLaunchKernelGGL(kernel, dim3((unsigned)((c.tiles + a.req.n_requests) * a.cache.kv_heads)), dim3(kSharedWaves * 64), lds, st, a, c.rows, (int)c.tiles);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((c.tiles + a.req.n_requests) * a.cache.kv_heads)), dim3(kSharedThreads), lds, st, a, c.rows, (int)c.tiles);
         } else if (c.team == 1)
             hipLaunchKernelGGL((spd_paged_selected_kernel<T, D, 1>), dim3((unsigned)((segments + kNarrowWaves - 1) / kNarrowWaves)),
                                dim3(kNarrowWaves * 64), 0, st, a, s, 1, c.head_tiles);

@@ -474,6 +474,40 @@ def test_sparse_tokens_that_share_pages_that_are_not_there(spd, h):
     assert_close(w, (out, lse), w.attention(selected=want), "shared pages that are not there")
 
 
+@pytest.mark.parametrize("group,kv_heads,n_select,dtype,dim,page,layout", [
+    (1, 16, 8, "bf16", 64, 16, "thd"), (3, 16, 8, "f16", 128, 32, "htd"), (4, 16, 8, "bf16", 128, 64, "thd"), (5, 16, 8, "bf16", 64, 64, "htd"),
+    (8, 16, 8, "f16", 64, 16, "thd"), (16, 8, 20, "bf16", 128, 16, "thd")])
+def test_sparse_tokens_that_meet_in_pages(spd, h, group, kv_heads, n_select, dtype, dim, page, layout):
+    """Tokens and key heads enough that a page is read once for all that chose it, with tiles of tokens that end inside a request or hold one token."""
+    w = World([(7 * page + 5, 203), (0, 1), (6, 130), (0, 0), (2 * page - 1, 65)], group=group, kv_heads=kv_heads, dtype=dtype, dim=dim,
+              page=page, layout=layout, seed=group, drift=0.7, fused=True)
+    print("meet", group, kv_heads, n_select, dtype, dim, page, flush=True)
+    check_sparse(spd, h, w, n_select, "pages that tokens meet in")
+
+
+def test_sparse_tokens_that_meet_in_large_pages(spd, h):
+    w = World([(2000, 600), (500, 31)], group=4, kv_heads=8, page=1024, seed=3, drift=0.7)
+    check_sparse(spd, h, w, 3, "pages of 1,024 that tokens meet in")
+
+
+def test_sparse_tokens_that_meet_in_a_long_request(spd, h):
+    """More pages than are marked at a time."""
+    w = World([(16 * 1030 + 3, 256)], group=8, kv_heads=32, dim=64, page=16, seed=4, drift=0.7)
+    check_sparse(spd, h, w, 64, "a long request that tokens meet in")
+
+
+def test_sparse_tokens_that_meet_in_pages_that_are_not_there(spd, h):
+    w = World([(100, 300), (40, 150), (10, 30)], group=4, kv_heads=16, page=16, seed=6, drift=0.7)
+    w.make_bounds()
+    w.table[0, [0, 3, 17, 21]] = torch.tensor([-1, w.pages, 2 ** 31 - 1, -(2 ** 31)], dtype=torch.int32)
+    w.table[1, 2] = -5
+    w.kv_lens[2] = 17                                   # fewer than there are new tokens
+    out, lse, selected = h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 9)
+    want = w.selection(9)
+    assert torch.equal(selected.cpu(), want)
+    assert_close(w, (out, lse), w.attention(selected=want), "pages that are not there")
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def serve(spd, h, steps, seed, n_select=0):
