@@ -91,9 +91,10 @@ struct Candidate { uint32_t key; int32_t page; };
 // once for all tokens of the workgroup.  The scores stay in LDS as keys, and a wavefront chooses for each token.  Where a
 // request has more pages, every 2,048 give their n_select best, and spd_paged_select_join_kernel chooses among those.
 // Bound by latency: one token over 470 pages 9 us (round trips for lengths, page numbers, queries and codes, then the search), 32 requests of up to 938 pages
-// 20 us, 2,048 tokens over 440 to 470 pages 51 us, half of it the search: 20 of its steps of 9 counts.
+// 20 us, 2,048 tokens over 440 to 470 pages 38 us, half of it the search: 20 of its steps of 9 counts.  Two workgroups share a compute unit,
+// which takes 64 registers a lane: with codes two steps ahead there were 74, and 51 us.
 template <spd_dtype T, int D>
-__global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const PagedAttention a, int32_t *const selected, Candidate *const candidates,
+__global__ void __launch_bounds__(kSelectThreads, 8) spd_paged_select_kernel(const PagedAttention a, int32_t *const selected, Candidate *const candidates,
                                                                            const int blocks, const int room) {
     using H = half_t<T>;
     constexpr int kSteps = 2 * D / 64, E = D / 64;
@@ -110,7 +111,7 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
     if (most > a.n_select) {
         const int low = lane & 15, quad = lane >> 4;
         const int32_t *const table = a.req.block_table + (int64_t)tile.request * a.req.table_stride + page0;
-        // A wavefront's page numbers, 4 steps' to a load, then the codes of two steps, on their way while the queries are.
+        // A wavefront's page numbers, 4 steps' to a load, then the codes of a step, on their way while the queries are.
         constexpr int kStride = kSelectTokens * 16, kRounds = kSelectPages / kStride / 4;
         int32_t numbers[kRounds];
 #pragma unroll
@@ -118,26 +119,25 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
             const int p = wave * 16 + (i * 4 + quad) * kStride + low;
             numbers[i] = p < pages ? table[p] : -1;
         }
-        struct Codes { i32x4 c[kSteps]; float scale; } codes[2];
-        auto fetch = [&](int step, Codes &to) {
+        struct Codes { i32x4 c[kSteps]; float scale; } codes;
+        auto fetch = [&](int step) {
             int number = -1;
 #pragma unroll
             for (int i = 0; i < kRounds; ++i) if (step >> 2 == i) number = __shfl(numbers[i], (step & 3) * 16 + low);
             const bool there = number >= 0 && number < a.cache.n_pages;
             const int64_t at = (int64_t)(there ? number : 0) * a.cache.kv_heads + kvh;
-            to.scale = -__builtin_inff();                         // (marks a page that is not there)
+            codes.scale = -__builtin_inff();                         // (marks a page that is not there)
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) to.c[s] = i32x4{0, 0, 0, 0};
+            for (int s = 0; s < kSteps; ++s) codes.c[s] = i32x4{0, 0, 0, 0};
             if (there) {
                 const int8_t *const from = a.cache.codes + at * 2 * D + quad * 16;
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) to.c[s] = *(const i32x4 *)(from + s * 64);
-                to.scale = a.cache.code_scale[at];
+                for (int s = 0; s < kSteps; ++s) codes.c[s] = *(const i32x4 *)(from + s * 64);
+                codes.scale = a.cache.code_scale[at];
             }
         };
         const int steps = pages > wave * 16 ? (pages - wave * 16 + kStride - 1) / kStride : 0;
-        if (steps > 0) fetch(0, codes[0]);
-        if (steps > 1) fetch(1, codes[1]);
+        if (steps > 0) fetch(0);
         if (wave < tile.count) {
             const H *const q = (const H *)a.q.ptr + (int64_t)(tile.first + wave) * a.q.token_stride + (int64_t)kvh * group * a.q.head_stride + lane * E;
             constexpr int kHeld = 8;                              // heads that stay in registers between the two passes
@@ -185,13 +185,13 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) q[s] = *(const i32x4 *)&s_code[low][s * 64 + quad * 16];
         const int own = low < tile.count && position0 + low >= 0 ? (position0 + low) >> shift : -1;    // of token `low`
-        auto score = [&](int step, Codes &of) {
+        for (int step = 0; step < steps; ++step) {
             const int p0 = wave * 16 + step * kStride;
             i32x4 x = {0, 0, 0, 0};
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_i32_16x16x64_i8(of.c[s], q[s], x, 0, 0, 0);
-            const float scale = of.scale;
-            if (step + 2 < steps) fetch(step + 2, of);
+            for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_i32_16x16x64_i8(codes.c[s], q[s], x, 0, 0, 0);
+            const float scale = codes.scale;
+            if (step + 1 < steps) fetch(step + 1);
             uint32_t key[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -202,10 +202,6 @@ __global__ void __launch_bounds__(kSelectThreads) spd_paged_select_kernel(const 
                 if (p > own) key[i] = 0;
             }
             *(uint4 *)&s_key[low * room + p0 + quad * 4] = make_uint4(key[0], key[1], key[2], key[3]);
-        };
-        for (int step = 0; step < steps; step += 2) {
-            score(step, codes[0]);
-            if (step + 1 < steps) score(step + 1, codes[1]);
         }
         __syncthreads();
     }
