@@ -1,4 +1,4 @@
-"""spd: sparse all-pairs distances as a semiring product on one MI355X (gfx950).
+"""spd: sparse all-pairs distances as a semiring product on one MI355X (gfx950), and attention over a paged cache.
 
 The package is a thin binding over ``libspd.so`` (built from ``csrc/`` by ``build.py``);
 ``paper_2104_06357_amd.testing`` holds the host-only hooks the tests use.

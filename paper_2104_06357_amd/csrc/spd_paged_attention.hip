@@ -194,7 +194,7 @@ struct PagePlaces {
 // takes them, a row's maximum and sum are a lane's (of four that share the keys), and V is read transposed from rows as they lie in memory.
 // Bound by the reading: 48 requests of 500 to 16,000 tokens, 64 heads on 8 of 128, 0.92 GB in 175 us, 5.2 TB/s (a large copy moves 4.95); one
 // request of 2,000 tokens, 8 MB, takes 13 us, most of it the way to its first keys (lengths, table, keys: three round trips).
-// Selected pages that many tokens share come out of L2: 2,048 tokens x 8 heads x 16 pages of 64, 8.6 GB in 440 us, 20 TB/s.  K went straight from
+// Selected pages come out of L2 where several tokens chose them: 2,048 tokens x 8 heads x 16 pages of 64, 8.6 GB in 405 us, 21 TB/s.  K went straight from
 // memory into the product's operand at first: a row to a lane then, which the vector caches answer with 64 lookups a load where this way has 16.
 
 constexpr int kNarrowRows = 16, kNarrowKeys = 32, kNarrowWaves = 4;
@@ -657,7 +657,10 @@ __global__ void __launch_bounds__(64) spd_paged_selected_join_kernel(const Paged
 // is read once for all.  A workgroup has a key head and 16 tiles of tokens, each as many as 16 rows hold; it marks in LDS which tiles' tokens chose
 // which page, lists the pages that anybody chose, and goes through them 64 keys a block.  4 wavefronts move the blocks into a ring of 128 KB, 8 with two
 // tiles each take part in those that their tokens chose, and each goes on as far as the ring lets it: with a barrier after every 128 keys all of them waited
-// for the one that had the most to do.  Windows of 512 pages, since marks take 32 bytes a page.
+// for the one that had the most to do (2,048 tokens, 32 heads on 8 of 128, 16 of 470 pages of 64: 362 us, and 240 this way).  Windows of 512 pages, since
+// marks take 32 bytes a page.
+// Bound by how far the ring lets the readers part (with half of it 311 us): 64 tokens choose 257 of the pages, and a reader takes some 50 for either
+// tile.  Moving alone takes 162 us (2.1 GB from L2), taking alone 245, and LDS is busy for 90 of them.
 constexpr int kSharedTiles = 16, kSharedReaders = 8, kSharedMovers = 4, kSharedPages = 512, kSharedThreads = (kSharedReaders + kSharedMovers) * 64;
 template <int D> struct SharedShape {
     static constexpr int kHalf = 32 * D * 2, kBlock = 4 * kHalf, kRing = 128 * 1024 / kBlock;      // bytes of 32 keys' K or V, and of a block: K, then V
@@ -893,7 +896,7 @@ __global__ void __launch_bounds__(kSharedThreads) spd_paged_shared_kernel(const 
 // ---- many rows: a workgroup to 128 or 256 of them ------------------------------------------------
 // Prompts: a wavefront has 32 rows, a workgroup's share what is read of K and V, 64 keys a unit, in LDS twice; registers hold the next unit. The
 // products are as above, 32 x 32 of them.  Bound by both kinds of arithmetic, which hardly overlap: with heads of 128 the matrix units are busy for
-// 47 % of the cycles and the vector units for 42 %.  8,192 tokens after 8,192, 32 heads on 8 of 128: 1.61 ms, 1.02 PFLOP/s (a
+// 47 % of the cycles and the vector units for 44 %.  8,192 tokens after 8,192, 32 heads on 8 of 128: 1.61 to 1.70 ms, 1.0 PFLOP/s (a
 // large matrix product reaches 1.58).  Tried and not kept: 64 rows to a wavefront and one of them to a SIMD (3.9 ms: every wait is exposed);
 // a half of the wavefronts half a unit behind the others (1.66); priorities for the products and units of 128 keys (no gain).  Heads of 64 are
 // bound by the exponentials and what goes with them, half the products to each; three workgroups of 4 wavefronts to a compute unit do better there
