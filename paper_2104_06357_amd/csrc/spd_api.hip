@@ -2084,6 +2084,7 @@ spd_status spd_paged_workspace_bytes(const spd_handle *h, const spd_paged_cache 
         b->n_requests > kPagedMostRequests || n_heads > 65535 || b->n_tokens >= kPagedMost / n_heads || b->max_pages >= kPagedMost / c->page_size)
         return SPD_ERR_UNSUPPORTED;
     if (n_select != 0 && (n_select < 2 || n_select > SPD_PAGED_MAX_SELECT)) return SPD_ERR_BAD_K;
+    if (n_select > 0 && b->n_tokens * n_heads > kPagedMostSelecting) return SPD_ERR_UNSUPPORTED;
     PagedAttention a = paged_attention_args(*c, *b, n_heads);
     a.n_select = n_select;
     a.selected = n_select > 0 ? reinterpret_cast<const int32_t *>(bytes) : nullptr;      // (only looked at for being there)

@@ -508,6 +508,45 @@ def test_sparse_tokens_that_meet_in_pages_that_are_not_there(spd, h):
     assert_close(w, (out, lse), w.attention(selected=want), "pages that are not there")
 
 
+def test_sparse_tokens_that_meet_with_lengths_that_contradict_the_arrays(spd, h):
+    """Requests that overlap, descend or end past the rows where tokens share pages: never an access outside, and the handle goes on."""
+    for starts in ([0, 400, 0, 400, 0], [0, 300, 100, 350, 400], [-7, 100, 100, 5000, 400], [400, 300, 200, 100, 0]):
+        w = World([(50, 1)] * 4, group=4, kv_heads=16, dim=64, seed=21)
+        w.make_bounds()
+        w.query_start = torch.tensor(starts, dtype=torch.int32)
+        w.q, w.tokens = torch.zeros((400, 64, 64), dtype=torch.bfloat16), 400
+        print("contradicting", starts, flush=True)
+        h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 3)
+        torch.cuda.synchronize()
+    w = World([(7 * 64 + 5, 203), (6, 130)], kv_heads=16, page=64, seed=22, drift=0.7)
+    w.kv_lens[1] = -4
+    w.make_bounds()
+    first = [x.clone() for x in h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 8)]
+    want = w.selection(8)
+    assert torch.equal(first[2].cpu(), want)
+    assert_close(w, first[:2], w.attention(selected=want), "a negative length where tokens meet")
+    for _ in range(5):                                  # whoever of the wavefronts was first
+        again = h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 8)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_sparse_tokens_that_meet_with_large_logits(spd, h):
+    """As test_attention_of_large_logits, where tokens share pages: the maximum moves late and differs from row to row."""
+    w = World([(400, 300)], group=4, kv_heads=16, page=32, seed=12)
+    for number, j in ((int(w.table[0, j]), j) for j in range(pages_of(700, 32))):
+        w.k[number] = (w.k[number].float() * (0.2 + 0.25 * j)).to(w.k.dtype)
+    w.make_bounds()
+    out, lse, selected = h.paged_sparse_attention(w.cache(spd), w.queries(), w.batch(spd), 10)
+    chosen = w.selection(10)
+    assert torch.equal(selected.cpu(), chosen)
+    want, want_lse, room = w.attention(selected=chosen)
+    out, lse = out.double().cpu(), lse.double().cpu()
+    # logits reach ~100: 128 products of fp32 sums are off by up to 128 * 2^-24 * sum |q k| <= 128 * 2^-24 * 900
+    tol = 128 * 2.0 ** -24 * 900
+    assert float((lse - want_lse).abs().max()) <= tol
+    assert bool(((out - want).abs() <= (2.0 ** -8 + tol) * (room + want.abs()) + 1e-12).all())
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def serve(spd, h, steps, seed, n_select=0):
@@ -676,6 +715,26 @@ def test_refusals_of_the_library(spd, h):
         h.set_workspace(None)
     assert need > 0
     assert_close(w, h.paged_attention(cache, q, batch), w.attention(), "after the refusals")
+
+
+def test_refusals_of_sizes(spd, h):
+    """More than a launch can deal out, or than 32 bits count: refused by the sizes alone."""
+    def refused(status, f):
+        with pytest.raises(spd.SpdError) as e:
+            f()
+        assert e.value.status_name == status and str(e.value), (status, e.value)
+
+    cache = spd.PagedCache(*(torch.zeros((4, 16, 8, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = spd.PagedBatch(i32([0, 1]), i32([1]), i32([[0]]))
+    row = torch.zeros((1, 8, 64), dtype=torch.bfloat16, device="cuda")
+    n = (1 << 25) + 1
+    refused("SPD_ERR_UNSUPPORTED", lambda: h.paged_append(cache, row.expand(n, 8, 64), row.expand(n, 8, 64), torch.full((n,), -1, device="cuda")))
+    for tokens, heads, select, status in ((1 << 31, 8, 0, "SPD_ERR_UNSUPPORTED"), (1 << 62, 8, 0, "SPD_ERR_UNSUPPORTED"), (1 << 26, 32, 0, "SPD_ERR_UNSUPPORTED"),
+                                          (1, 8, 65, "SPD_ERR_BAD_K"), (1, 8, 1, "SPD_ERR_BAD_K"), (1, 12, 0, "SPD_ERR_DIM_MISMATCH"),
+                                          (1 << 23, 16, 4, "SPD_ERR_UNSUPPORTED")):
+        refused(status, lambda: h.paged_workspace_bytes(cache, batch, tokens, heads, select))
+    assert h.paged_workspace_bytes(cache, batch, 1 << 20, 8) > 0
 
 
 def test_scratch_of_the_callers(spd):
